@@ -319,6 +319,86 @@ int32_t citrus_decode_step(const citrus_config* cfg, citrus_tensor q, citrus_ten
                            void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * Generation with drafts: every document of the batch proposes a tree of up to 64 tokens, all of them attend at once over the
+ * document's cache and their own ancestors, and the path that the model accepts is then put into the cache (citrus_tree_commit).
+ *   out[b,l,h,t,:] = sum_j softmax_j(scale * q[b,l,h,t,:] . K_j) * V_j    over the states j that node t of document b sees:
+ *   cache rows 0 .. len_b - 1, and draft row u iff bit u of ancestors[b * ancestors_stride_b + t] is set.
+ * A node sees itself: a word whose own bit t is clear says that there is no node t in this document (the trees of a batch differ
+ * in size); such a row of out is zero and its lse -infinity, whatever q holds there.  Bits from draft_len on are ignored.  What
+ * a node does not see does not touch its row, be it infinite or NaN.  A draft of one token with the word 1 is a decoding step
+ * for documents of different lengths.
+ *
+ * q, out             [B, L, Hq, draft_len, d]; 1 <= draft_len <= 64; out must not overlap an input
+ * k_draft, v_draft   [B, L, Hkv, draft_len, d]: the nodes' own states (nothing is appended to the cache)
+ * ancestors          device, 8-byte aligned; ancestors_stride_b words from one document to the next: >= draft_len, or 0
+ *                    where all documents share one tree
+ * k_cache, v_cache   [B, L, Hkv, >= cache_len, d]   (ptr may be NULL iff cache_len == 0)
+ * cache_len          0 .. cfg->cache_capacity
+ * cache_lens         optional, device int32 [B]: the documents' lengths, 0 .. cache_len (values outside are taken as the
+ *                    nearest of these); NULL: cache_len for all.  Rows from a document's length on are not read into its result.
+ * lse                optional, dense [B, L, Hq, draft_len] f32: log-sum-exp of each row's scaled logits
+ * workspace          >= citrus_generation_workspace_bytes(cfg, draft_len)
+ * Compute: as citrus_chunk_attn; row sums in f32.
+ */
+int32_t citrus_tree_attn(const citrus_config* cfg, citrus_tensor q, citrus_tensor k_draft, citrus_tensor v_draft, int32_t draft_len,
+                         const uint64_t* ancestors, int64_t ancestors_stride_b, citrus_tensor k_cache, citrus_tensor v_cache,
+                         int32_t cache_len, const int32_t* cache_lens, citrus_tensor out, float* lse, void* workspace,
+                         size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The accepted path of a draft joins the cache, in place and each document its own number of tokens: for i < accepted[b]
+ *   cache row len_b + i = draft row path[b, i]     of K and of V, in every layer and head; bit copies.
+ * Rows from len_b + accepted[b] on are left as they were.
+ *
+ * k_draft, v_draft   [B, L, Hkv, draft_len, d]; 1 <= draft_len <= 64; must not overlap the caches
+ * path               device, dense int32 [B, path_len]: node numbers 0 .. draft_len - 1 from the root on; 1 <= path_len <= 64.  A
+ *                    number outside leaves its cache row as it was.
+ * accepted           device int32 [B], 0 .. path_len (values outside are taken as the nearest of these; no row is written
+ *                    past cfg->cache_capacity)
+ * k_cache, v_cache   [B, L, Hkv, cache_capacity, d], in/out
+ * cache_len, cache_lens  as in citrus_tree_attn
+ * new_lens           optional, device int32 [B], out: len_b + accepted[b], at most cache_capacity; another array than cache_lens,
+ *                    accepted and path
+ */
+int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citrus_tensor v_draft, int32_t draft_len,
+                           const int32_t* path, int32_t path_len, const int32_t* accepted, citrus_tensor k_cache,
+                           citrus_tensor v_cache, int32_t cache_len, const int32_t* cache_lens, int32_t* new_lens, void* hip_stream);
+
+/*
+ * Generation in bounded memory: one decoding step, after which the state that has received the least attention makes room
+ * (the accumulative-attention rule of H2O, Section 5.2 "Baselines", while the response is generated; the chunk loop's ACCUMULATED
+ * score mode is the same rule for the instruction's scores, and its sums may be passed on here).  With n = min(tokens, budget) states
+ * in the cache, the token attends over them and itself:
+ *   out[b,l,h,0,:] = sum_j p[h,j] * V_j,  p[h,:] = softmax(scale * q[b,l,h,0,:] . K),   w[g,j] = sum_{h in g} p[h,j]
+ *   acc[b,l,g,j] += w[g,j] for the n states
+ * tokens < budget: the token's state becomes row n, and its sum is its own weight w.
+ * Otherwise the cache is full.  Its last `recent` rows hold the newest states in turn, row
+ *   r = budget - recent + (tokens - budget) mod recent
+ * the oldest of them.  Of rows start_size .. budget - recent - 1 and r, the one with the smallest sum goes (of equal ones the lowest; a
+ * sum that is NaN is never the smallest, and r goes if there is no smaller one); state r, unless it is the one that goes, moves to that
+ * row with its sum; the token's state and weight become row r.  (Two rows are written however long the cache is: attention does not
+ * depend on the order of its states.)  With start_size + recent == budget this is a sliding window behind the first states.
+ * cfg->select_mode PER_LAYER: one row for all KV heads of a layer, by the sum of their sums in head order.
+ *
+ * q, out         [B, L, Hq, 1, d];  k_new, v_new  [B, L, Hkv, 1, d]: the token's own state; out must not overlap an input
+ * k_cache, v_cache [B, L, Hkv, >= min(tokens + 1, budget), d], in/out
+ * acc            dense f32 [B, L, Hkv, cache_capacity], in/out: the states' sums
+ * tokens         states that have been put into this cache so far, evicted ones included; the caller's count becomes tokens + 1.  A
+ *                cache filled otherwise (by the chunk loop) starts with its number of states.
+ * recent         1 .. budget - start_size; the same in every step
+ * evicted        optional, device, dense int32 [B, L, Hsel]: the row whose state went, -1 while the cache grows
+ * workspace      >= citrus_generation_workspace_bytes(cfg, 1)
+ * Weights and sums are f32 in both types.
+ */
+int32_t citrus_decode_evict_step(const citrus_config* cfg, citrus_tensor q, citrus_tensor k_new, citrus_tensor v_new,
+                                 citrus_tensor k_cache, citrus_tensor v_cache, float* acc, int32_t tokens, int32_t recent,
+                                 citrus_tensor out, int32_t* evicted, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Bytes of workspace that are enough for citrus_tree_attn with up to draft_len nodes and for citrus_decode_evict_step under this
+ * configuration (0 if cfg is NULL or invalid, or draft_len not in 1 .. 64). */
+size_t citrus_generation_workspace_bytes(const citrus_config* cfg, int32_t draft_len);
+
+/*
  * The two steps of the ACCUMULATED score mode around the selection (Section 5.2, H2O's accumulative
  * attention score on the instruction-aware cache):
  *   citrus_score_accumulate  score[b,l,g,j] += acc[b,l,g,j] for j < cache_len: a cache state's sum so far is

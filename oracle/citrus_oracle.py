@@ -40,6 +40,11 @@ What each function follows in the paper:
   states (Section 4.3): the new token's state joins the cache and its query
   attends over all of it, the same softmax attention as in Eq. (1).
 
+* ``decode_evict_step``: the same step in bounded memory: the token's attention
+  weights join the states' sums and the state with the smallest sum goes (the
+  accumulative-attention rule of H2O, Section 5.2 "Baselines").
+* ``tree_attn``: the attention of the same step for a tree of drafted tokens.
+
 Readings taken where the paper is silent (all listed again in the design
 notes of the repository):
 
@@ -543,6 +548,73 @@ def decode_step(q_new, k_new, v_new, k_cache, v_cache, scale: Optional[float] = 
         p, _ = softmax_rows((k_all[g] @ q_new[h])[None, :] * sc)
         out[h] = p[0] @ v_all[g]
     return out, k_all, v_all
+
+
+def tree_attn(q, k_draft, v_draft, ancestors: Sequence[int], k_cache, v_cache, scale: Optional[float] = None):
+    """Attention of the nodes of a drafted tree over one document's cache (all of its rows) and the nodes' ancestors.
+
+    q [Hq, T, d], k_draft / v_draft [Hkv, T, d], k_cache / v_cache [Hkv, n, d]; bit u of ancestors[t]: node t sees node u.
+    A word without its own bit says that there is no such node: its row is zero, its log-sum-exp -inf.
+    Returns (out [Hq, T, d], lse [Hq, T], magnitude [Hq, T, d] = sum_j p_j |v_j|: what roundings of p and v scale with).
+    """
+    q, k_draft, v_draft, k_cache, v_cache = (_f64(x) for x in (q, k_draft, v_draft, k_cache, v_cache))
+    hq, nodes, d = q.shape
+    group = hq // k_draft.shape[0]
+    sc = _scale(d, scale)
+    out, mag = np.zeros_like(q), np.zeros_like(q)
+    lse = np.full((hq, nodes), -np.inf)
+    for h in range(hq):
+        g = h // group
+        for t in range(nodes):
+            if not ancestors[t] >> t & 1:
+                continue
+            seen = [u for u in range(nodes) if ancestors[t] >> u & 1]
+            keys = np.concatenate([k_cache[g], k_draft[g][seen]])
+            values = np.concatenate([v_cache[g], v_draft[g][seen]])
+            s = keys @ q[h, t] * sc
+            e = np.exp(s - s.max())
+            lse[h, t] = s.max() + np.log(e.sum())
+            out[h, t] = (e / e.sum()) @ values
+            mag[h, t] = (e / e.sum()) @ np.abs(values)
+    return out, lse, mag
+
+
+def decode_evict_step(q_new, k_new, v_new, k_cache, v_cache, acc, tokens: int, budget: int, recent: int, start_size: int = 0,
+                      select_mode: int = SELECT_PER_KV_HEAD, scale: Optional[float] = None, forced=None):
+    """One decoding step in a cache of at most `budget` states that evicts by accumulated attention weight (the rule of H2O,
+    Section 5.2 "Baselines", during generation).
+
+    q_new [Hq, d], k_new / v_new [Hkv, d]; k_cache / v_cache [Hkv, n, d] and acc [Hkv, n] with n = min(tokens, budget).
+    forced: the row to evict per KV head (a caller replays another selection), else the smallest sum, the lowest row of equal ones.
+    Returns (out [Hq, d], sums [Hkv, n + 1] before anything moves, evicted rows per KV head or None, k, v, acc after the step).
+    """
+    q_new, k_new, v_new, k_cache, v_cache, acc = (_f64(x) for x in (q_new, k_new, v_new, k_cache, v_cache, acc))
+    hkv, n, d = k_cache.shape
+    assert n == min(tokens, budget)
+    group = q_new.shape[0] // hkv
+    k = np.concatenate([k_cache, k_new[:, None]], axis=1)
+    v = np.concatenate([v_cache, v_new[:, None]], axis=1)
+    sums = np.concatenate([acc, np.zeros((hkv, 1))], axis=1)
+    out = np.zeros_like(q_new)
+    for h in range(q_new.shape[0]):
+        p = softmax_rows((k[h // group] @ q_new[h] * _scale(d, scale))[None])[0][0]
+        out[h] = p @ v[h // group]
+        sums[h // group] += p
+    if tokens < budget:
+        return out, sums, None, k, v, sums.copy()
+    oldest = budget - recent + (tokens - budget) % recent
+    rank = np.repeat(sums.sum(axis=0)[None], hkv, axis=0) if select_mode == SELECT_PER_LAYER else sums
+    evicted = np.zeros(hkv, dtype=np.int64)
+    k_after, v_after, acc_after = k[:, :n].copy(), v[:, :n].copy(), sums[:, :n].copy()
+    for g in range(hkv):
+        best = oldest
+        for j in list(range(start_size, budget - recent)) + [oldest]:
+            if rank[g, j] < rank[g, best] or (rank[g, j] == rank[g, best] and j < best):
+                best = j
+        evicted[g] = best if forced is None else forced[g]
+        for dst, src in ((evicted[g], oldest), (oldest, n)):
+            k_after[g, dst], v_after[g, dst], acc_after[g, dst] = k[g, src], v[g, src], sums[g, src]
+    return out, sums, evicted, k_after, v_after, acc_after
 
 
 def full_causal_attention(q, k, v, scale: Optional[float] = None) -> np.ndarray:

@@ -32,7 +32,8 @@ OK, ERR_NULL, ERR_SHAPE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_DEVICE, ERR_PROVIDE
 EXPORTS = (
     "citrus_abi_version", "citrus_status_string", "citrus_workspace_bytes", "citrus_chunk_attn",
     "citrus_instr_score", "citrus_cache_score", "citrus_evict_cache", "citrus_evict_cache_static",
-    "citrus_static_scratch_bytes", "citrus_decode_step", "citrus_rope", "citrus_score_accumulate", "citrus_score_gather", "citrus_topk_select", "citrus_kv_compact", "citrus_resident_provider",
+    "citrus_static_scratch_bytes", "citrus_decode_step", "citrus_tree_attn", "citrus_tree_commit", "citrus_decode_evict_step",
+    "citrus_generation_workspace_bytes", "citrus_rope", "citrus_score_accumulate", "citrus_score_gather", "citrus_topk_select", "citrus_kv_compact", "citrus_resident_provider",
     "citrus_process_document", "citrus_probe_mfma",
 )
 
@@ -105,6 +106,14 @@ def _lib():
     lib.citrus_static_scratch_bytes.argtypes = []
     lib.citrus_decode_step.restype = I
     lib.citrus_decode_step.argtypes = [P(CConfig), CTensor, CTensor, CTensor, CTensor, CTensor, I, CTensor, V, S, V]
+    lib.citrus_tree_attn.restype = I
+    lib.citrus_tree_attn.argtypes = [P(CConfig), CTensor, CTensor, CTensor, I, V, C.c_int64, CTensor, CTensor, I, V, CTensor, V, V, S, V]
+    lib.citrus_tree_commit.restype = I
+    lib.citrus_tree_commit.argtypes = [P(CConfig), CTensor, CTensor, I, V, I, V, CTensor, CTensor, I, V, V, V]
+    lib.citrus_decode_evict_step.restype = I
+    lib.citrus_decode_evict_step.argtypes = [P(CConfig), CTensor, CTensor, CTensor, CTensor, CTensor, V, I, I, CTensor, V, V, S, V]
+    lib.citrus_generation_workspace_bytes.restype = S
+    lib.citrus_generation_workspace_bytes.argtypes = [P(CConfig), I]
     lib.citrus_rope.restype = I
     lib.citrus_rope.argtypes = [P(CConfig), CTensor, I, I, I, CTensor, V]
     lib.citrus_score_accumulate.restype = I
@@ -314,6 +323,130 @@ def citrus_decode_step(cfg: Config, q, k_new, v_new, k_cache, v_cache, cache_len
                                    tensor(v_cache), cache_len, tensor(out), _ptr(workspace),
                                    0 if workspace is None else workspace.numel(), _stream(stream))
     _check(st, "citrus_decode_step")
+    return out
+
+
+def generation_workspace_bytes(cfg: Config, draft_len: int = 1) -> int:
+    cc = cfg.c()
+    return int(_lib().citrus_generation_workspace_bytes(C.byref(cc), draft_len))
+
+
+def alloc_generation_workspace(cfg: Config, draft_len: int = 1, device="cuda") -> torch.Tensor:
+    """For citrus_tree_attn with up to draft_len nodes and for citrus_decode_evict_step."""
+    n = generation_workspace_bytes(cfg, draft_len)
+    if n == 0:
+        raise CitrusError(ERR_SHAPE, "citrus_generation_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _states(what: str, t, cfg: Config, heads: int, rows: int, device: int, at_least: bool = False) -> CTensor:
+    """citrus_tensor of t, which has to be [B, L, heads, rows (or more), d] of the configuration's type on `device`."""
+    shape = t.shape
+    if (len(shape) != 5 or shape[0] != cfg.batch or shape[1] != cfg.layers or shape[2] != heads or shape[4] != cfg.head_dim or
+            (shape[3] < rows if at_least else shape[3] != rows)):
+        raise ValueError(f"{what}: shape {tuple(shape)}, expected {(cfg.batch, cfg.layers, heads, rows, cfg.head_dim)}" +
+                         (" with that many rows or more" if at_least else ""))
+    if t.dtype is not (torch.float32 if cfg.dtype == F32 else torch.bfloat16):
+        raise ValueError(f"{what}: {t.dtype}, the configuration has {cfg.torch_dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{what}: on another device than the first tensor")
+    return tensor(t)
+
+
+def _dense(what: str, t, dtype, shape: tuple, device: int) -> Optional[int]:
+    """Address of t, which has to be a dense tensor of this type and shape on `device`; None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: {t.dtype} of shape {tuple(t.shape)}, expected a dense {dtype} of {shape}")
+    if t.get_device() != device:
+        raise ValueError(f"{what}: on another device than the first tensor")
+    return t.data_ptr()
+
+
+def _on(device: int):
+    """The device that a call's tensors are on has to be the current one: its stream and its kernels are used."""
+    if device < 0 or device != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {'the host' if device < 0 else f'device {device}'}, not on the current device")
+
+
+def _generation_block(workspace, device: int):
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace: a dense tensor on the device of the others is needed")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def citrus_tree_attn(cfg: Config, q, k_draft, v_draft, ancestors, k_cache, v_cache, cache_len: int, cache_lens=None, out=None,
+                     lse=None, workspace=None, stream=None):
+    """Attention of drafted trees q [B, L, Hq, nodes, d] over the caches and the nodes' ancestors: ancestors is int64
+    [B, nodes], or [nodes] for one tree in all documents, bit u of a node's word for node u, its own among them (without it there is no
+    such node).  cache_lens: int32 [B] lengths of the documents, up to cache_len.  Returns out."""
+    nodes, device = q.shape[3], q.get_device()
+    _on(device)
+    hq, hkv = cfg.q_heads, cfg.kv_heads
+    if out is None:
+        out = torch.empty_like(q)
+    shared = ancestors.dim() == 1
+    cached = cache_len > 0 or k_cache is not None or v_cache is not None
+    cc = cfg.c()
+    block, size = _generation_block(workspace, device)
+    st = _lib().citrus_tree_attn(
+        C.byref(cc), _states("q", q, cfg, hq, nodes, device), _states("k_draft", k_draft, cfg, hkv, nodes, device),
+        _states("v_draft", v_draft, cfg, hkv, nodes, device), nodes,
+        _dense("ancestors", ancestors, torch.int64, (nodes,) if shared else (cfg.batch, nodes), device), 0 if shared else nodes,
+        _states("k_cache", k_cache, cfg, hkv, cache_len, device, True) if cached else tensor(None),
+        _states("v_cache", v_cache, cfg, hkv, cache_len, device, True) if cached else tensor(None), cache_len,
+        _dense("cache_lens", cache_lens, torch.int32, (cfg.batch,), device), _states("out", out, cfg, hq, nodes, device),
+        _dense("lse", lse, torch.float32, (cfg.batch, cfg.layers, hq, nodes), device), block, size, _stream(stream))
+    _check(st, "citrus_tree_attn")
+    return out
+
+
+def citrus_tree_commit(cfg: Config, k_draft, v_draft, path, accepted, k_cache, v_cache, cache_len: int, cache_lens=None,
+                       new_lens=None, stream=None):
+    """Puts the draft states path[b, :accepted[b]] behind the cache of every document b, in place; path int32 [B, path_len],
+    accepted and cache_lens int32 [B].  Returns new_lens [B], the documents' new lengths."""
+    nodes, device, hkv = k_draft.shape[3], k_draft.get_device(), cfg.kv_heads
+    _on(device)
+    if new_lens is None:
+        new_lens = torch.empty(cfg.batch, dtype=torch.int32, device=k_draft.device)
+    path_len = path.shape[1] if path.dim() == 2 else 0
+    rows = cfg.cache_capacity
+    cc = cfg.c()
+    st = _lib().citrus_tree_commit(
+        C.byref(cc), _states("k_draft", k_draft, cfg, hkv, nodes, device), _states("v_draft", v_draft, cfg, hkv, nodes, device),
+        nodes, _dense("path", path, torch.int32, (cfg.batch, path_len), device), path_len,
+        _dense("accepted", accepted, torch.int32, (cfg.batch,), device), _states("k_cache", k_cache, cfg, hkv, rows, device, True),
+        _states("v_cache", v_cache, cfg, hkv, rows, device, True), cache_len,
+        _dense("cache_lens", cache_lens, torch.int32, (cfg.batch,), device),
+        _dense("new_lens", new_lens, torch.int32, (cfg.batch,), device), _stream(stream))
+    _check(st, "citrus_tree_commit")
+    return new_lens
+
+
+def citrus_decode_evict_step(cfg: Config, q, k_new, v_new, k_cache, v_cache, acc, tokens: int, recent: int, out=None, evicted=None,
+                             workspace=None, stream=None):
+    """One decoding step in a cache of at most cfg.budget states: the token's weights join the states' sums acc
+    [B, L, Hkv, cache_capacity], and in a full cache the state with the smallest sum makes room (the last `recent` rows, the newest
+    states, and the first cfg.start_size are kept).  tokens: states put into the cache so far.  Updates the caches and acc in place;
+    evicted: int32 [B, L, sel_heads], the row whose state went, or -1.  Returns out."""
+    device, hq, hkv = q.get_device(), cfg.q_heads, cfg.kv_heads
+    _on(device)
+    if out is None:
+        out = torch.empty_like(q)
+    rows = min(tokens + 1, cfg.budget)
+    cc = cfg.c()
+    block, size = _generation_block(workspace, device)
+    st = _lib().citrus_decode_evict_step(
+        C.byref(cc), _states("q", q, cfg, hq, 1, device), _states("k_new", k_new, cfg, hkv, 1, device),
+        _states("v_new", v_new, cfg, hkv, 1, device), _states("k_cache", k_cache, cfg, hkv, rows, device, True),
+        _states("v_cache", v_cache, cfg, hkv, rows, device, True),
+        _dense("acc", acc, torch.float32, (cfg.batch, cfg.layers, hkv, cfg.cache_capacity), device), tokens, recent,
+        _states("out", out, cfg, hq, 1, device), _dense("evicted", evicted, torch.int32, (cfg.batch, cfg.layers, cfg.sel_heads), device),
+        block, size, _stream(stream))
+    _check(st, "citrus_decode_evict_step")
     return out
 
 

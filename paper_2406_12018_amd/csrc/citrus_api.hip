@@ -382,6 +382,47 @@ StaticEvictLayout static_evict_layout(const citrus_config* c, int rows, int cach
   return s;
 }
 
+// ---- generation: what a workspace of citrus_generation_workspace_bytes holds ----
+struct EvictStepLayout {
+  size_t scores, lse2, own, best, attn, total;
+  int64_t score_pitch;
+};
+EvictStepLayout evict_step_layout(const citrus_config* c) {
+  const size_t units_q = static_cast<size_t>(c->batch) * c->layers * c->q_heads;
+  const size_t units_kv = static_cast<size_t>(c->batch) * c->layers * c->kv_heads;
+  EvictStepLayout w;
+  w.score_pitch = (static_cast<int64_t>(c->budget) + 1 + 31) / 32 * 32;
+  size_t off = 0;
+  w.scores = off; off += align_up(units_q * w.score_pitch * sizeof(float));
+  w.lse2 = off;   off += align_up(units_q * sizeof(float));
+  w.own = off;    off += align_up(units_kv * sizeof(float));
+  w.best = off;   off += align_up(units_kv * evict_step_ranges(c->budget) * 2 * sizeof(float));
+  w.attn = off;   off += align_up(few_rows_workspace_floats(c->dtype, dims_of(c), 1) * sizeof(float));
+  w.total = off;
+  return w;
+}
+size_t generation_bytes(const citrus_config* c, int draft_len) {
+  const size_t tree = align_up(few_rows_workspace_floats(c->dtype, dims_of(c), draft_len) * sizeof(float));
+  const size_t evict = evict_step_layout(c).total;
+  return tree > evict ? tree : evict;
+}
+citrus_status check_generation_workspace(const citrus_config* c, int draft_len, const void* ws, size_t bytes) {
+  if (ws == nullptr || bytes < generation_bytes(c, draft_len)) return CITRUS_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(ws) % 16 != 0) return CITRUS_ERR_WORKSPACE;
+  return CITRUS_OK;
+}
+template <typename T>
+bool misaligned(const T* p) { return reinterpret_cast<uintptr_t>(p) % sizeof(T) != 0; }
+citrus_status check_draft(const citrus_config* c, int draft_len, int cache_len, const citrus_tensor& k_draft, const citrus_tensor& v_draft,
+                          const citrus_tensor& k_cache, const citrus_tensor& v_cache, const int32_t* cache_lens) {
+  if (draft_len < 1 || draft_len > kMaxNodes) return CITRUS_ERR_SHAPE;
+  if (cache_len < 0 || cache_len > c->cache_capacity || misaligned(cache_lens)) return CITRUS_ERR_SHAPE;
+  CITRUS_TRY(check_tensor(c, k_draft, draft_len, false));
+  CITRUS_TRY(check_tensor(c, v_draft, draft_len, false));
+  if (k_draft.ptr == k_cache.ptr || v_draft.ptr == v_cache.ptr) return CITRUS_ERR_SHAPE;
+  return CITRUS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -540,6 +581,103 @@ int32_t citrus_decode_step(const citrus_config* cfg, citrus_tensor q, citrus_ten
                                    /*appended=*/1,
                                    make_view(rows_from(k_cache, cache_len, cfg->dtype)),
                                    make_view(rows_from(v_cache, cache_len, cfg->dtype)), nullptr, 0, nullptr, 0, st));
+}
+
+size_t citrus_generation_workspace_bytes(const citrus_config* cfg, int32_t draft_len) {
+  if (check_config(cfg) != CITRUS_OK || draft_len < 1 || draft_len > kMaxNodes) return 0;
+  return generation_bytes(cfg, draft_len);
+}
+
+int32_t citrus_tree_attn(const citrus_config* cfg, citrus_tensor q, citrus_tensor k_draft, citrus_tensor v_draft, int32_t draft_len,
+                         const uint64_t* ancestors, int64_t ancestors_stride_b, citrus_tensor k_cache, citrus_tensor v_cache,
+                         int32_t cache_len, const int32_t* cache_lens, citrus_tensor out, float* lse, void* workspace,
+                         size_t workspace_bytes, void* hip_stream) {
+  CITRUS_TRY(check_config(cfg));
+  CITRUS_TRY(check_draft(cfg, draft_len, cache_len, k_draft, v_draft, k_cache, v_cache, cache_lens));
+  if (ancestors == nullptr) return CITRUS_ERR_NULL;
+  if (misaligned(ancestors) || misaligned(lse) || (ancestors_stride_b != 0 && ancestors_stride_b < draft_len)) return CITRUS_ERR_SHAPE;
+  CITRUS_TRY(check_tensor(cfg, q, draft_len, false));
+  CITRUS_TRY(check_tensor(cfg, out, draft_len, false));
+  CITRUS_TRY(check_tensor(cfg, k_cache, cache_len, cache_len == 0));
+  CITRUS_TRY(check_tensor(cfg, v_cache, cache_len, cache_len == 0));
+  if (out.ptr == q.ptr) return CITRUS_ERR_SHAPE;
+  CITRUS_TRY(check_generation_workspace(cfg, draft_len, workspace, workspace_bytes));
+  FewRows a{};
+  a.dm = dims_of(cfg);
+  a.q = make_view(q);
+  a.ks = segments(k_cache, cache_len, k_draft, draft_len);
+  a.vs = segments(v_cache, cache_len, v_draft, draft_len);
+  a.lens = cache_lens;
+  a.words = ancestors;
+  a.words_sb = ancestors_stride_b;
+  a.out = make_view(out);
+  a.lse = lse;
+  a.workspace = static_cast<float*>(workspace);
+  return hip_status(launch_few_rows(cfg->dtype, a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citrus_tensor v_draft, int32_t draft_len,
+                           const int32_t* path, int32_t path_len, const int32_t* accepted, citrus_tensor k_cache,
+                           citrus_tensor v_cache, int32_t cache_len, const int32_t* cache_lens, int32_t* new_lens, void* hip_stream) {
+  CITRUS_TRY(check_config(cfg));
+  CITRUS_TRY(check_draft(cfg, draft_len, cache_len, k_draft, v_draft, k_cache, v_cache, cache_lens));
+  if (path == nullptr || accepted == nullptr) return CITRUS_ERR_NULL;
+  if (path_len < 1 || path_len > kMaxNodes || misaligned(path) || misaligned(accepted) || misaligned(new_lens)) return CITRUS_ERR_SHAPE;
+  CITRUS_TRY(check_tensor(cfg, k_cache, cfg->cache_capacity, false));
+  CITRUS_TRY(check_tensor(cfg, v_cache, cfg->cache_capacity, false));
+  if (new_lens != nullptr && (new_lens == cache_lens || new_lens == accepted || new_lens == path)) return CITRUS_ERR_SHAPE;
+  const Commit a{path, accepted, cache_lens, new_lens, path_len, draft_len, cache_len, cfg->cache_capacity};
+  return hip_status(launch_tree_commit(elem_bytes(cfg->dtype), dims_of(cfg), make_view(k_draft), make_view(v_draft), make_view(k_cache),
+                                       make_view(v_cache), a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int32_t citrus_decode_evict_step(const citrus_config* cfg, citrus_tensor q, citrus_tensor k_new, citrus_tensor v_new,
+                                 citrus_tensor k_cache, citrus_tensor v_cache, float* acc, int32_t tokens, int32_t recent,
+                                 citrus_tensor out, int32_t* evicted, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  CITRUS_TRY(check_config(cfg));
+  if (tokens < 0 || recent < 1 || recent > cfg->budget - cfg->start_size) return CITRUS_ERR_SHAPE;
+  if (acc == nullptr) return CITRUS_ERR_NULL;
+  if (misaligned(acc) || misaligned(evicted)) return CITRUS_ERR_SHAPE;
+  const bool full = tokens >= cfg->budget;
+  const int n = full ? cfg->budget : tokens, rows = full ? n : n + 1;
+  CITRUS_TRY(check_tensor(cfg, q, 1, false));
+  CITRUS_TRY(check_tensor(cfg, k_new, 1, false));
+  CITRUS_TRY(check_tensor(cfg, v_new, 1, false));
+  CITRUS_TRY(check_tensor(cfg, k_cache, rows, false));
+  CITRUS_TRY(check_tensor(cfg, v_cache, rows, false));
+  CITRUS_TRY(check_tensor(cfg, out, 1, false));
+  if (k_new.ptr == k_cache.ptr || v_new.ptr == v_cache.ptr || out.ptr == q.ptr) return CITRUS_ERR_SHAPE;
+  CITRUS_TRY(check_generation_workspace(cfg, 1, workspace, workspace_bytes));
+  const EvictStepLayout wl = evict_step_layout(cfg);
+  char* ws = static_cast<char*>(workspace);
+  FewRows a{};
+  a.dm = dims_of(cfg);
+  a.q = make_view(q);
+  a.ks = segments(k_cache, n, k_new, 1);
+  a.vs = segments(v_cache, n, v_new, 1);
+  a.out = make_view(out);
+  a.scores = reinterpret_cast<float*>(ws + wl.scores);
+  a.score_pitch = wl.score_pitch;
+  a.lse2 = reinterpret_cast<float*>(ws + wl.lse2);
+  a.workspace = reinterpret_cast<float*>(ws + wl.attn);
+  EvictStep e{};
+  e.dm = a.dm;
+  e.n = n;
+  e.start = cfg->start_size;
+  e.recent = recent;
+  e.oldest = full ? n - recent + (tokens - n) % recent : -1;
+  e.acc = acc;
+  e.acc_pitch = cfg->cache_capacity;
+  e.scores = a.scores;
+  e.score_pitch = wl.score_pitch;
+  e.lse2 = a.lse2;
+  e.own = reinterpret_cast<float*>(ws + wl.own);
+  e.best = reinterpret_cast<float2*>(ws + wl.best);
+  e.evicted = evicted;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  CITRUS_TRY(hip_status(launch_few_rows(cfg->dtype, a, st)));
+  return hip_status(launch_evict_step(elem_bytes(cfg->dtype), e, cfg->select_mode == CITRUS_SELECT_PER_LAYER, make_view(k_new),
+                                      make_view(v_new), make_view(k_cache), make_view(v_cache), st));
 }
 
 int32_t citrus_score_accumulate(const citrus_config* cfg, float* score, int32_t n, const float* acc,

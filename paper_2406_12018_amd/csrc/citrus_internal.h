@@ -138,6 +138,52 @@ size_t decode_mfma_workspace_floats(const Dims& dm);
 hipError_t launch_decode_mfma(const Dims& dm, View q, Segments kseg, Segments vseg, View out, float* workspace,
                               int append_token, hipStream_t st);
 
+// ---- generation: a few query rows per head over a cache and ks.c <= 64 states of their own, tree_attn.hip ----
+constexpr int kMaxNodes = 64;
+struct FewRows {
+  Dims dm;
+  View q;
+  Segments ks, vs;        // n_c: the cache's rows, or the most a document may have
+  const int32_t* lens;    // optional [B]: the documents' own
+  const uint64_t* words;  // optional: bit u of words[b * words_sb + t] says that row t sees state u of its own
+  int64_t words_sb;
+  View out;
+  float* lse;             // optional [B, L, Hq, c]: natural logarithm ...
+  float* lse2;            // ... and base 2
+  float* scores;          // optional [B, L, Hq][score_pitch] (c == 1): the logits, base 2
+  int64_t score_pitch;
+  float* workspace;       // few_rows_workspace_floats
+};
+size_t few_rows_workspace_floats(int dtype, const Dims& dm, int rows);  // for any call with at most `rows` rows per head
+hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t st);
+
+struct Commit {
+  const int32_t *path, *accepted, *lens;  // [B][path_len], [B], optional [B]
+  int32_t* new_lens;                      // optional [B]
+  int path_len, nodes, cache_len, capacity;
+};
+hipError_t launch_tree_commit(int elem_bytes, const Dims& dm, View k_draft, View v_draft, View k_cache, View v_cache,
+                              const Commit& a, hipStream_t st);
+
+// ---- generation: the states' sums of attention weights and the state that makes room, evict_step.hip ----
+struct EvictStep {
+  Dims dm;
+  int n;                 // cached states
+  int start, recent;     // the slots that are kept, at the front and at the end, ...
+  int oldest;            // ... but for this one of the latter; -1: the cache grows
+  float* acc;            // [B, L, Hkv][acc_pitch]
+  int64_t acc_pitch;
+  const float* scores;   // [B, L, Hq][score_pitch], base 2, the token's own behind the n states'
+  int64_t score_pitch;
+  const float* lse2;     // [B, L, Hq]
+  float* own;            // [B, L, Hkv]: the token's weight
+  float2* best;          // [B, L, Hkv][ranges of keys]
+  int32_t* evicted;      // optional [B, L, Hsel]
+};
+int evict_step_ranges(int n);
+hipError_t launch_evict_step(int elem_bytes, const EvictStep& a, bool per_layer, View k_new, View v_new, View k_cache,
+                             View v_cache, hipStream_t st);
+
 // ---- rotary embedding at explicit positions, rope.hip ----
 // y[b,l,h,s,:] = RoPE(x[b,l,h,s,:], pos0 + s) for h < heads, s < rows; y may be x itself.
 hipError_t launch_rope(int dtype, const Dims& dm, View x, View y, int heads, int rows, int pos0, float base,
