@@ -156,6 +156,8 @@ struct FewRows {
 };
 size_t few_rows_workspace_floats(int dtype, const Dims& dm, int rows);  // for any call with at most `rows` rows per head
 hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t st);
+size_t few_rows_bf16_workspace_floats(const Dims& dm, int rows);  // few_rows_bf16.hip
+hipError_t launch_few_rows_bf16(const FewRows& a, hipStream_t st);
 
 struct Commit {
   const int32_t *path, *accepted, *lens;  // [B][path_len], [B], optional [B]

@@ -1,0 +1,501 @@
+// Attention of a few query rows per KV head in bf16: the nodes of drafted trees, single tokens of documents of different lengths, and
+// the tokens of a bounded cache, whose logits are kept.
+//
+// Up to 32 rows a KV head, the launch is the stream of K/V bytes; the matrix pipe then has 1 to 2 KB of LDS tile per MFMA and is
+// idle most of the time.  With R rows of a head group a byte of K/V meets R flop, and from about R = 256 on the matrix pipe
+// bounds.  Two forms of one kernel:
+//   PRIVATE  up to 32 rows: every wave streams 32-key tiles of its own through LDS, with no barrier between the waves;
+//   shared   more rows: the waves of a workgroup read the same 64-key stages, four of them in LDS, a block of 32 rows per KH waves
+//            (KH = 2: each takes half of a stage's keys), one barrier a stage.
+// Keys are split over workgroups where the units do not fill the chip, and few_rows_merge_kernel joins the ranges.
+#include "key_stream.h"
+
+namespace citrus {
+namespace {
+
+typedef __attribute__((address_space(3))) void* lds_void_ptr;
+typedef __attribute__((address_space(3))) char* lds_char_ptr;
+
+constexpr int kStageKeys = 64, kStages = 4;  // shared form
+constexpr int kMostSplits = 64;
+
+// Results of a range of keys: {maximum (base 2), sum} and the row before its division.
+struct Partials {
+  float2* ml;  // [range][B*L*Hq*T]
+  float* o;    // [range][B*L*Hq*T][D]
+};
+
+// What the lanes of one query row hold of it.
+template <int D>
+struct Column {
+  float m = -INFINITY, l = 0.f;  // running maximum (base 2), this lane's part of the sum
+  f32x16 o[Geo<D>::kOut];
+};
+
+// Zero, unless one of the words is infinite or NaN: those times zero are NaN.  One instruction per two values.
+__device__ inline float zero_if_finite(const Pack8& a, float sum) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a.w[i]), __builtin_bit_cast(bf16x2, 0u), sum, false);
+  return sum;
+}
+
+// Four elements of a row's result.  m: the maximum its sum was formed with.
+__device__ inline void finish_row(const FewRows& a, int b, int l, int h, int t, int64_t row, int d, float m, float sum, const float (&o)[4]) {
+  const bool real = a.words == nullptr || (a.words[b * a.words_sb + t] >> t & 1);
+  uint2 w = {0, 0};
+  if (real) {
+    w.x = pack_bf16x2(o[0] / sum, o[1] / sum);
+    w.y = pack_bf16x2(o[2] / sum, o[3] / sum);
+  }
+  *reinterpret_cast<uint2*>(const_cast<uint16_t*>(row_ptr<uint16_t>(a.out, b, l, h, t)) + d) = w;
+  if (d == 0) {
+    const float lse2 = real ? m + log2f(sum) : -INFINITY;
+    if (a.lse != nullptr) a.lse[row] = lse2 * kLn2;
+    if (a.lse2 != nullptr) a.lse2[row] = lse2;
+  }
+}
+
+// vmcnt(LEFT), nothing else
+template <int LEFT>
+__device__ inline void wait_loads() {
+  static_assert(LEFT < 64);
+  __builtin_amdgcn_s_waitcnt((LEFT & 15) | 7 << 4 | 15 << 8 | (LEFT >> 4) << 14);
+  asm volatile("" ::: "memory");
+}
+
+// One 32-key tile.  LAST: keys that not every row sees; bit j of `seen` says that this lane's row sees key j of the tile.
+// PARTS: bf16 words of a weight in P.V.
+template <int D, int PARTS, bool LAST>
+__device__ __forceinline__ void key_tile(uint32_t k_t, uint32_t v_t, const uint32_t (&k_off)[Geo<D>::kKk], const uint32_t (&v_off)[2 * Geo<D>::kOut],
+                                         const bf16x8 (&q_op)[Geo<D>::kKk], float c2, uint32_t seen, Column<D>& c, float* scores) {
+  typedef Geo<D> T;
+  const int lane = threadIdx.x % 64, col = lane % 32, grp = lane / 32;
+  f32x16 s_acc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s_acc[i] = 0.f;
+  {
+    Pack8 a[T::kKk];
+    uint32_t addr[T::kKk];
+#pragma unroll
+    for (int kk = 0; kk < T::kKk; ++kk) addr[kk] = k_t + k_off[kk];
+    lds_read_k_operands(a, addr);
+#pragma unroll
+    for (int kk = 0; kk < T::kKk; ++kk) s_acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[kk].v, q_op[kk], s_acc, 0, 0, 0);
+  }
+  if constexpr (LAST) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (!(seen >> (8 * (i / 4) + 4 * grp + i % 4) & 1)) s_acc[i] = -INFINITY;
+  }
+  if (scores != nullptr) {
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4)
+      *reinterpret_cast<float4*>(scores + 8 * i4 + 4 * grp) =
+          make_float4(s_acc[4 * i4] * c2, s_acc[4 * i4 + 1] * c2, s_acc[4 * i4 + 2] * c2, s_acc[4 * i4 + 3] * c2);
+  }
+  float mx = s_acc[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s_acc[i]);
+  if (__any(mx * c2 > c.m + kMaxSlack)) {  // the maximum moves only when some row's did by more than that
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float m_new = fmaxf(c.m, mx * c2);
+    const float alpha = __builtin_amdgcn_exp2f(c.m - (m_new == -INFINITY ? 0.f : m_new));  // 0 on the first tile
+    c.l *= alpha;
+#pragma unroll
+    for (int r = 0; r < T::kOut; ++r)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) c.o[r][i] *= alpha;
+    c.m = m_new;
+  }
+  const float m_use = LAST && c.m == -INFINITY ? 0.f : c.m;  // a row that has not seen a state yet
+  float p[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s_acc[i], c2, -m_use));
+  uint32_t p_pk[PARTS][8];
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (PARTS == 2)
+      split_bf16x2(p[2 * i], p[2 * i + 1], p_pk[0][i], p_pk[1][i]);
+    else
+      p_pk[0][i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
+    sum += p[2 * i] + p[2 * i + 1];
+  }
+  c.l += sum;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    Pack8 av[T::kOut];
+    {
+      uint32_t addr[2 * T::kOut];
+#pragma unroll
+      for (int e = 0; e < 2 * T::kOut; ++e) addr[e] = v_t + 16 * half * T::kRowBytes + v_off[e];
+      lds_read_v_operands(av, addr);
+    }
+    if constexpr (LAST || PARTS == 2) {
+      // 0 x infinity is NaN: a value that some row does not see, or the second part of a weight that one part holds.  Values that
+      // are infinite or NaN are taken out of the operands and their products added one by one, to the rows that see them: what
+      // a row does not see leaves the bits of its result alone.
+      float zero = 0.f;
+#pragma unroll
+      for (int r = 0; r < T::kOut; ++r) zero = zero_if_finite(av[r], zero);
+      if (__any(zero != 0.f)) {
+#pragma unroll 1
+        for (int key = 16 * half; key < 16 * half + 16; ++key) {
+          const int at = 4 * (key / 8) + key % 4;
+          float pk = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) pk = at == i ? p[i] : pk;
+          pk = __shfl(pk, col + 32 * (key / 4 % 2), 64);
+          const bool sees = !LAST || (seen >> key & 1);
+#pragma unroll
+          for (int r = 0; r < T::kOut; ++r)
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) {
+              const int c0 = 8 * i4 + 4 * grp, d = 16 * r + c0 % 16 + D / 2 * (c0 / 16);
+              const uint32_t addr = v_t + key * T::kRowBytes + ((d / 8) ^ T::swz(key)) * 16 + d % 8 * 2;
+              i32x2 w;
+              asm volatile("ds_read_b64 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(w) : "v"(addr) : "memory");
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const float v = __uint_as_float(x % 2 ? w[x / 2] & 0xffff0000u : static_cast<uint32_t>(w[x / 2]) << 16);
+                if (sees && !(fabsf(v) < INFINITY)) c.o[r][4 * i4 + x] = fmaf(pk, v, c.o[r][4 * i4 + x]);
+              }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < T::kOut; ++r)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t w = av[r].w[i];
+            if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+            if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
+            av[r].w[i] = w;
+          }
+      }
+    }
+#pragma unroll
+    for (int y = 0; y < PARTS; ++y) {
+      Pack8 pb;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) pb.w[x] = p_pk[y][4 * half + x];
+#pragma unroll
+      for (int r = 0; r < T::kOut; ++r) c.o[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[r].v, pb.v, c.o[r], 0, 0, 0);
+    }
+  }
+}
+
+// grid: (row groups * Hkv * key ranges, B * L)
+template <int D, int WAVES, int KH, int PARTS, bool SCORES>
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, int key_splits, Partials part) {
+  typedef Geo<D> T;
+  constexpr bool kPrivate = KH == WAVES;
+  constexpr int kBlocks = WAVES / KH;  // of 32 rows
+  constexpr int kTileBytes = T::kTileBytes, kR = T::kRowsPerLoad;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const Dims& dm = a.dm;
+  const int lane = threadIdx.x % 64, col = lane % 32, grp = lane / 32;
+  const int wu = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int sp = blockIdx.x % key_splits, g = blockIdx.x / key_splits % dm.Hkv, row_group = blockIdx.x / key_splits / dm.Hkv;
+  const int b = blockIdx.y / dm.L, l = blockIdx.y % dm.L;
+  const int nodes = a.ks.c, rows = dm.G * nodes;
+  const int n_c = a.lens != nullptr ? min(max(a.lens[b], 0), a.ks.n_c) : a.ks.n_c;
+  const int n = n_c + nodes;
+
+  // this lane's row: node t of head h
+  const int row = (row_group * kBlocks + wu / KH) * 32 + col;
+  const int h = g * dm.G + min(row, rows - 1) / nodes, t = min(row, rows - 1) % nodes;
+  uint64_t word = a.words != nullptr ? a.words[b * a.words_sb + t] : 1;
+  if (nodes < 64) word &= (uint64_t{1} << nodes) - 1;
+  const bool idle = (row_group * kBlocks + wu / KH) * 32 >= rows;  // a wave without rows helps to load
+
+  const int k_ss_cache = static_cast<int>(a.ks.cache.ss), k_ss_own = static_cast<int>(a.ks.chunk.ss);
+  const int v_ss_cache = static_cast<int>(a.vs.cache.ss), v_ss_own = static_cast<int>(a.vs.chunk.ss);
+  auto resource = [&](const View& v, int count, int ss) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(row_ptr<uint16_t>(v, b, l, g, 0)), 0,
+                                             count > 0 ? ((count - 1) * ss + D) * 2 : 0, kBufferFlags);
+  };
+  const __amdgpu_buffer_rsrc_t k_rs_cache = resource(a.ks.cache, n_c, k_ss_cache), k_rs_own = resource(a.ks.chunk, nodes, k_ss_own);
+  const __amdgpu_buffer_rsrc_t v_rs_cache = resource(a.vs.cache, n_c, v_ss_cache), v_rs_own = resource(a.vs.chunk, nodes, v_ss_own);
+  const int fill_row = lane / T::kSegs, fill_pos = lane % T::kSegs;
+  // rows j0 + kR i + (0 .. kR - 1), kR rows from `first` on, to K rows at k_t and V rows at v_t.  Past the last state: the last.
+  auto fill = [&](int j0, int first, int count, char* k_t, char* v_t) {
+    const bool in_cache = j0 + kR * (first + count) <= n_c;
+#pragma unroll
+    for (int i = first; i < first + count; ++i) {
+      const int r = kR * i + fill_row;
+      const int seg = (fill_pos ^ T::swz(r)) * 16;
+      const lds_void_ptr kd = (lds_void_ptr)(k_t + kR * i * T::kRowBytes), vd = (lds_void_ptr)(v_t + kR * i * T::kRowBytes);
+      if (in_cache) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rs_cache, kd, 16, (j0 + r) * k_ss_cache * 2 + seg, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rs_cache, vd, 16, (j0 + r) * v_ss_cache * 2 + seg, 0, 0, 0);
+      } else {  // two predicated loads: a resource chosen per lane would be loaded in a serialising loop
+        const int j = min(j0 + r, n - 1);
+        if (j < n_c) {
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rs_cache, kd, 16, j * k_ss_cache * 2 + seg, 0, 0, 0);
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rs_cache, vd, 16, j * v_ss_cache * 2 + seg, 0, 0, 0);
+        }
+        keep_apart();
+        if (j >= n_c) {
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rs_own, kd, 16, (j - n_c) * k_ss_own * 2 + seg, 0, 0, 0);
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rs_own, vd, 16, (j - n_c) * v_ss_own * 2 + seg, 0, 0, 0);
+        }
+        keep_apart();
+      }
+    }
+  };
+  const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char_ptr)lds));
+
+  // per-lane LDS read offsets inside a tile, swizzle included
+  uint32_t k_off[T::kKk], v_off[2 * T::kOut];
+#pragma unroll
+  for (int kk = 0; kk < T::kKk; ++kk) k_off[kk] = col * T::kRowBytes + (((2 * kk + grp) ^ T::swz(col)) * 16);
+  const int s16 = lane % 16, q16 = lane / 16;
+  const int v_cl = (T::kSegs / 2 * (q16 % 2) + (s16 % 4) / 2) ^ T::swz(4 * (q16 / 2) + s16 / 4);
+#pragma unroll
+  for (int e = 0; e < 2 * T::kOut; ++e) v_off[e] = (4 * (q16 / 2) + s16 / 4) * T::kRowBytes + ((e ^ v_cl) * 16) + 8 * (s16 % 2);
+
+  bf16x8 q_op[T::kKk];
+  {
+    const uint16_t* qp = row_ptr<uint16_t>(a.q, b, l, h, t) + 8 * grp;
+#pragma unroll
+    for (int kk = 0; kk < T::kKk; ++kk) {
+      Pack8 x;
+      x.u = *reinterpret_cast<const uint4*>(qp + 16 * kk);
+      q_op[kk] = x.v;
+    }
+  }
+  wait_loads<0>();  // the operand has landed before the first tile is asked for
+
+  const float c2 = dm.scale * kLog2e;
+  Column<D> c;
+#pragma unroll
+  for (int r = 0; r < T::kOut; ++r)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) c.o[r][i] = 0.f;
+  float* scores = nullptr;
+  if constexpr (SCORES)
+    if (row < rows) scores = a.scores + (static_cast<int64_t>(blockIdx.y) * dm.Hq + h) * a.score_pitch;
+
+  auto tile = [&](int j0, uint32_t k_t, uint32_t v_t) {
+    float* const s = SCORES && scores != nullptr ? scores + j0 : nullptr;
+    const int own = j0 - n_c;  // of the tile's first key
+    if (own + 32 <= 0) {
+      key_tile<D, PARTS, false>(k_t, v_t, k_off, v_off, q_op, c2, 0, c, s);
+    } else {
+      const uint32_t seen = own >= 0 ? static_cast<uint32_t>(word >> own)
+                                     : static_cast<uint32_t>(word) << -own | ((1u << -own) - 1);
+      key_tile<D, PARTS, true>(k_t, v_t, k_off, v_off, q_op, c2, seen, c, s);
+    }
+  };
+
+  if constexpr (kPrivate) {
+    // key tiles of this workgroup's range, dealt to its waves in turn
+    const int tiles = (n + 31) / 32, per = (tiles + key_splits - 1) / key_splits;
+    const int end = min(tiles, (sp + 1) * per);
+    char* const mine = lds + wu * T::kWaveLdsBytes;  // [buffer][K | V][tile]
+    const uint32_t mine_at = lds_at + wu * T::kWaveLdsBytes;
+    auto fill_tile = [&](int x, int buf) {
+      char* k_t = mine + buf * 2 * kTileBytes;
+      fill(x * 32, 0, 32 / kR, k_t, k_t + kTileBytes);
+    };
+    int x = sp * per + wu;
+    if (x < end) fill_tile(x, 0);
+    for (int it = 0; x < end; x += WAVES, ++it) {
+      const int buf = it & 1;
+      // the other buffer was last read in the previous turn, whose reads have all returned
+      if (x + WAVES < end) {
+        fill_tile(x + WAVES, buf ^ 1);
+        wait_loads<T::kLoadsPerTile>();
+      } else {
+        wait_loads<0>();
+      }
+      const uint32_t k_t = mine_at + buf * 2 * kTileBytes;
+      tile(x * 32, k_t, k_t + kTileBytes);
+    }
+  } else {
+    constexpr int kSub = kStageKeys / 32, kStageBytes = 2 * kSub * kTileBytes, kGroups = kStageKeys / kR / WAVES;
+    constexpr int kLoads = 2 * kGroups;  // of a wave and stage, at least (the stage behind the cache's last row takes more)
+    static_assert(kGroups >= 1 && kSub % KH == 0);
+    const int stages = (n + kStageKeys - 1) / kStageKeys, per = (stages + key_splits - 1) / key_splits;
+    const int begin = sp * per, end = min(stages, begin + per);
+    auto fill_stage = [&](int x) {
+      char* k_t = lds + (x - begin) % kStages * kStageBytes;
+      fill(x * kStageKeys, wu * kGroups, kGroups, k_t, k_t + kSub * kTileBytes);
+    };
+    for (int x = begin; x < min(end, begin + kStages - 1); ++x) fill_stage(x);
+    for (int x = begin; x < end; ++x) {
+      // this wave's loads of the stage have landed; behind the barrier everybody's have, and the stage before has been read
+      if (x + kStages - 2 < end)
+        wait_loads<kLoads*(kStages - 2)>();
+      else
+        wait_loads<0>();
+      asm volatile("s_barrier" ::: "memory");
+      if (x + kStages - 1 < end) fill_stage(x + kStages - 1);
+      if (idle) continue;
+      const uint32_t k_t = lds_at + (x - begin) % kStages * kStageBytes, v_t = k_t + kSub * kTileBytes;
+#pragma unroll
+      for (int y = 0; y < kSub / KH; ++y) {
+        const int sub = KH == 1 ? y : wu % KH;
+        const int j0 = x * kStageKeys + 32 * sub;
+        if (j0 < n) tile(j0, k_t + sub * kTileBytes, v_t + sub * kTileBytes);
+      }
+    }
+  }
+
+  // ---- the waves of a block of rows join through LDS (the tiles have been read when every wave is here) ----
+  constexpr int kPitch = D + 4;
+  const float l_row = c.l + __shfl_xor(c.l, 32, 64);
+  __syncthreads();
+  float* const o_s = reinterpret_cast<float*>(lds);                                       // [wave][32 rows][kPitch]
+  float2* const ml_s = reinterpret_cast<float2*>(lds + WAVES * 32 * kPitch * sizeof(float));  // [wave][32]
+  if (row < rows) {
+    if (grp == 0) ml_s[wu * 32 + col] = make_float2(c.m, l_row);
+#pragma unroll
+    for (int r = 0; r < T::kOut; ++r)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        // registers 4 i4 .. + 3 are rows c' = 8 i4 + 4 grp + 0..3 of O^T -> head_dim 16 r + (c' % 16) + D / 2 (c' / 16)
+        const int c0 = 8 * i4 + 4 * grp;
+        *reinterpret_cast<float4*>(o_s + (wu * 32 + col) * kPitch + 16 * r + c0 % 16 + D / 2 * (c0 / 16)) =
+            make_float4(c.o[r][4 * i4], c.o[r][4 * i4 + 1], c.o[r][4 * i4 + 2], c.o[r][4 * i4 + 3]);
+      }
+  }
+  __syncthreads();
+  const int first = row_group * kBlocks * 32, here = min(kBlocks * 32, rows - first);
+  for (int e = threadIdx.x; e < here * (D / 4); e += 64 * WAVES) {
+    const int r = e / (D / 4), d = e % (D / 4) * 4;
+    const int at = (r / 32 * KH) * 32 + r % 32;
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < KH; ++w) m = fmaxf(m, ml_s[at + 32 * w].x);
+    const float m_use = m == -INFINITY ? 0.f : m;
+    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < KH; ++w) {
+      const float2 ml = ml_s[at + 32 * w];
+      const float wgt = __builtin_amdgcn_exp2f(ml.x - m_use);
+      const float4 x = *reinterpret_cast<const float4*>(o_s + (at + 32 * w) * kPitch + d);
+      sum = fmaf(ml.y, wgt, sum);
+      o[0] = fmaf(x.x, wgt, o[0]);
+      o[1] = fmaf(x.y, wgt, o[1]);
+      o[2] = fmaf(x.z, wgt, o[2]);
+      o[3] = fmaf(x.w, wgt, o[3]);
+    }
+    const int hq = g * dm.G + (first + r) / nodes, tt = (first + r) % nodes;
+    const int64_t at_row = (static_cast<int64_t>(blockIdx.y) * dm.Hq + hq) * nodes + tt;
+    if (key_splits == 1) {
+      finish_row(a, b, l, hq, tt, at_row, d, m_use, sum, o);
+    } else {
+      const int64_t p = static_cast<int64_t>(sp) * dm.B * dm.L * dm.Hq * nodes + at_row;
+      *reinterpret_cast<float4*>(part.o + p * D + d) = make_float4(o[0], o[1], o[2], o[3]);
+      if (d == 0) part.ml[p] = make_float2(m, sum);
+    }
+  }
+}
+
+// The ranges of keys join: one thread per four elements of a row.
+template <int D>
+__global__ __launch_bounds__(256) void few_rows_merge_kernel(FewRows a, int key_splits, Partials part) {
+  const Dims& dm = a.dm;
+  const int nodes = a.ks.c;
+  const int e = blockIdx.x * 256 + threadIdx.x;
+  if (e >= dm.Hq * nodes * (D / 4)) return;
+  const int d = e % (D / 4) * 4, r = e / (D / 4);
+  const int64_t all = static_cast<int64_t>(dm.B) * dm.L * dm.Hq * nodes, row = static_cast<int64_t>(blockIdx.y) * dm.Hq * nodes + r;
+  float m = -INFINITY;
+  for (int s = 0; s < key_splits; ++s) m = fmaxf(m, part.ml[s * all + row].x);
+  const float m_use = m == -INFINITY ? 0.f : m;
+  float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < key_splits; ++s) {
+    const float2 ml = part.ml[s * all + row];
+    const float wgt = __builtin_amdgcn_exp2f(ml.x - m_use);
+    const float4 x = *reinterpret_cast<const float4*>(part.o + (s * all + row) * D + d);
+    sum = fmaf(ml.y, wgt, sum);
+    o[0] = fmaf(x.x, wgt, o[0]);
+    o[1] = fmaf(x.y, wgt, o[1]);
+    o[2] = fmaf(x.z, wgt, o[2]);
+    o[3] = fmaf(x.w, wgt, o[3]);
+  }
+  finish_row(a, blockIdx.y / dm.L, blockIdx.y % dm.L, r / nodes, r % nodes, row, d, m_use, sum, o);
+}
+
+// How a call is launched.
+struct Plan {
+  int waves, kh, row_groups, splits;
+};
+// Ranges of keys.  A compute unit holds one workgroup (head_dim 64: two); rounds of the chip times a workgroup's share of the
+// keys is what the launch takes, and a second launch costs about as much as eight 32-key tiles of a workgroup's stream.
+Plan plan_for(const Dims& dm, int nodes, int most_keys, bool scores) {
+  const int blocks = (dm.G * nodes + 31) / 32;
+  Plan p;
+  p.waves = blocks <= 2 || scores ? 4 : 8;
+  p.kh = blocks == 1 || scores ? 4 : blocks <= 4 ? 2 : 1;
+  p.row_groups = (blocks + p.waves / p.kh - 1) / (p.waves / p.kh);
+  const int64_t groups = static_cast<int64_t>(dm.B) * dm.L * dm.Hkv * p.row_groups, slots = dm.D == 128 ? 256 : 512;
+  const int unit = p.kh == 4 ? 32 : kStageKeys, tiles = (most_keys + unit - 1) / unit;
+  int64_t best = INT64_MAX;
+  p.splits = 1;
+  for (int s = 1; s <= kMostSplits && s * groups <= 4 * slots; ++s) {
+    const int per = (tiles + s - 1) / s;
+    if (s > 1 && per * unit < 128) break;
+    if ((tiles + per - 1) / per != s) continue;  // no empty ranges
+    const int64_t cost = (s * groups + slots - 1) / slots * (per * unit / 32 + 6) + (s > 1 ? 8 : 0);
+    if (cost < best) best = cost, p.splits = s;
+  }
+  return p;
+}
+size_t partial_floats(const Dims& dm, int nodes, int splits) {
+  return splits == 1 ? 0 : static_cast<size_t>(splits) * dm.B * dm.L * dm.Hq * nodes * (dm.D + 2);
+}
+
+template <int D, int WAVES, int KH, int PARTS, bool SCORES>
+hipError_t launch(const FewRows& a, const Plan& p, const Partials& part, hipStream_t st) {
+  constexpr int kJoin = WAVES * 32 * ((D + 4) * 4 + 8);
+  constexpr int kTiles = KH == WAVES ? WAVES * Geo<D>::kWaveLdsBytes : kStages * (kStageKeys / 32) * 2 * Geo<D>::kTileBytes;
+  constexpr int kLds = kJoin > kTiles ? kJoin : kTiles;
+  static LdsLimit limit;
+  const auto kernel = few_rows_kernel<D, WAVES, KH, PARTS, SCORES>;
+  hipError_t e = raise_lds_limit(limit, reinterpret_cast<const void*>(kernel), kLds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3(p.row_groups * a.dm.Hkv * p.splits, a.dm.B * a.dm.L), dim3(64 * WAVES), kLds, st, a, p.splits, part);
+  return hipGetLastError();
+}
+template <int D>
+hipError_t launch_all(const FewRows& a, hipStream_t st) {
+  const Plan p = plan_for(a.dm, a.ks.c, a.ks.n_c + a.ks.c, a.scores != nullptr);
+  Partials part{nullptr, nullptr};
+  if (p.splits > 1) {
+    part.o = a.workspace;
+    part.ml = reinterpret_cast<float2*>(a.workspace + static_cast<size_t>(p.splits) * a.dm.B * a.dm.L * a.dm.Hq * a.ks.c * D);
+  }
+  hipError_t e = a.scores != nullptr ? launch<D, 4, 4, 2, true>(a, p, part, st)
+                 : p.kh == 4         ? launch<D, 4, 4, 2, false>(a, p, part, st)
+                 : p.waves == 4      ? launch<D, 4, 2, 2, false>(a, p, part, st)
+                 : p.kh == 2         ? launch<D, 8, 2, 2, false>(a, p, part, st)
+                                     : launch<D, 8, 1, D == 64 ? 2 : 1, false>(a, p, part, st);
+  if (e != hipSuccess || p.splits == 1) return e;
+  const int pieces = a.dm.Hq * a.ks.c * (D / 4);
+  hipLaunchKernelGGL(few_rows_merge_kernel<D>, dim3((pieces + 255) / 256, a.dm.B * a.dm.L), dim3(256), 0, st, a, p.splits, part);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t few_rows_bf16_workspace_floats(const Dims& dm, int rows) {
+  size_t most = 0;
+  for (int t = 1; t <= rows; ++t)
+    for (int scores = 0; scores < (t == 1 ? 2 : 1); ++scores) {
+      const int blocks = (dm.G * t + 31) / 32, kh = blocks == 1 || scores ? 4 : blocks <= 4 ? 2 : 1;
+      const int per = (blocks <= 2 || scores ? 4 : 8) / kh;
+      const int64_t groups = static_cast<int64_t>(dm.B) * dm.L * dm.Hkv * ((blocks + per - 1) / per), slots = dm.D == 128 ? 256 : 512;
+      const int64_t s = 4 * slots / groups;
+      const size_t f = partial_floats(dm, t, static_cast<int>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s));
+      if (f > most) most = f;
+    }
+  return most;
+}
+
+hipError_t launch_few_rows_bf16(const FewRows& a, hipStream_t st) { return a.dm.D == 128 ? launch_all<128>(a, st) : launch_all<64>(a, st); }
+
+}  // namespace citrus

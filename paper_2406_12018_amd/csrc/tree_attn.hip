@@ -105,13 +105,14 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(Dims dm, View kd, View
 
 }  // namespace
 
-size_t few_rows_workspace_floats(int, const Dims&, int) { return 0; }
+size_t few_rows_workspace_floats(int dtype, const Dims& dm, int rows) {
+  return dtype == CITRUS_BF16 ? few_rows_bf16_workspace_floats(dm, rows) : 0;
+}
 
 hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t st) {
+  if (dtype == CITRUS_BF16) return launch_few_rows_bf16(a, st);
   const dim3 grid((a.dm.Hq * a.ks.c + 3) / 4, a.dm.B * a.dm.L);
-  const bool wide = a.dm.D == 128;
-  const auto kernel = dtype == CITRUS_BF16 ? (wide ? few_rows_kernel<uint16_t, 128> : few_rows_kernel<uint16_t, 64>)
-                                           : (wide ? few_rows_kernel<float, 128> : few_rows_kernel<float, 64>);
+  const auto kernel = a.dm.D == 128 ? few_rows_kernel<float, 128> : few_rows_kernel<float, 64>;
   hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
