@@ -388,7 +388,7 @@ int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citr
  * recent         1 .. budget - start_size; the same in every step
  * evicted        optional, device, dense int32 [B, L, Hsel]: the row whose state went, -1 while the cache grows
  * workspace      >= citrus_generation_workspace_bytes(cfg, 1)
- * Weights and sums are f32 in both types.
+ * At most 1024 query heads per KV head, else CITRUS_ERR_UNSUPPORTED.  Weights and sums are f32 in both types.
  */
 int32_t citrus_decode_evict_step(const citrus_config* cfg, citrus_tensor q, citrus_tensor k_new, citrus_tensor v_new,
                                  citrus_tensor k_cache, citrus_tensor v_cache, float* acc, int32_t tokens, int32_t recent,

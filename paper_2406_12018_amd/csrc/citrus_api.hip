@@ -384,7 +384,7 @@ StaticEvictLayout static_evict_layout(const citrus_config* c, int rows, int cach
 
 // ---- generation: what a workspace of citrus_generation_workspace_bytes holds ----
 struct EvictStepLayout {
-  size_t scores, lse2, own, best, attn, total;
+  size_t scores, own, best, attn, total;
   int64_t score_pitch;
 };
 EvictStepLayout evict_step_layout(const citrus_config* c) {
@@ -394,7 +394,6 @@ EvictStepLayout evict_step_layout(const citrus_config* c) {
   w.score_pitch = (static_cast<int64_t>(c->budget) + 1 + 31) / 32 * 32;
   size_t off = 0;
   w.scores = off; off += align_up(units_q * w.score_pitch * sizeof(float));
-  w.lse2 = off;   off += align_up(units_q * sizeof(float));
   w.own = off;    off += align_up(units_kv * sizeof(float));
   w.best = off;   off += align_up(units_kv * evict_step_ranges(c->budget) * 2 * sizeof(float));
   w.attn = off;   off += align_up(few_rows_workspace_floats(c->dtype, dims_of(c), 1) * sizeof(float));
@@ -613,7 +612,7 @@ int32_t citrus_tree_attn(const citrus_config* cfg, citrus_tensor q, citrus_tenso
   a.out = make_view(out);
   a.lse = lse;
   a.workspace = static_cast<float*>(workspace);
-  return hip_status(launch_few_rows(cfg->dtype, a, static_cast<hipStream_t>(hip_stream)));
+  return hip_status(launch_tree_attn(cfg->dtype, a, static_cast<hipStream_t>(hip_stream)));
 }
 
 int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citrus_tensor v_draft, int32_t draft_len,
@@ -636,6 +635,7 @@ int32_t citrus_decode_evict_step(const citrus_config* cfg, citrus_tensor q, citr
                                  citrus_tensor out, int32_t* evicted, void* workspace, size_t workspace_bytes, void* hip_stream) {
   CITRUS_TRY(check_config(cfg));
   if (tokens < 0 || recent < 1 || recent > cfg->budget - cfg->start_size) return CITRUS_ERR_SHAPE;
+  if (cfg->q_heads / cfg->kv_heads > 1024) return CITRUS_ERR_UNSUPPORTED;
   if (acc == nullptr) return CITRUS_ERR_NULL;
   if (misaligned(acc) || misaligned(evicted)) return CITRUS_ERR_SHAPE;
   const bool full = tokens >= cfg->budget;
@@ -658,7 +658,6 @@ int32_t citrus_decode_evict_step(const citrus_config* cfg, citrus_tensor q, citr
   a.out = make_view(out);
   a.scores = reinterpret_cast<float*>(ws + wl.scores);
   a.score_pitch = wl.score_pitch;
-  a.lse2 = reinterpret_cast<float*>(ws + wl.lse2);
   a.workspace = reinterpret_cast<float*>(ws + wl.attn);
   EvictStep e{};
   e.dm = a.dm;
@@ -668,16 +667,15 @@ int32_t citrus_decode_evict_step(const citrus_config* cfg, citrus_tensor q, citr
   e.oldest = full ? n - recent + (tokens - n) % recent : -1;
   e.acc = acc;
   e.acc_pitch = cfg->cache_capacity;
-  e.scores = a.scores;
-  e.score_pitch = wl.score_pitch;
-  e.lse2 = a.lse2;
+  e.k_new = a.ks.chunk;
+  e.v_new = a.vs.chunk;
+  e.k_cache = make_view(k_cache);
+  e.v_cache = make_view(v_cache);
+  e.row_bytes = cfg->head_dim * elem_bytes(cfg->dtype);
+  e.evicted = evicted;
   e.own = reinterpret_cast<float*>(ws + wl.own);
   e.best = reinterpret_cast<float2*>(ws + wl.best);
-  e.evicted = evicted;
-  hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  CITRUS_TRY(hip_status(launch_few_rows(cfg->dtype, a, st)));
-  return hip_status(launch_evict_step(elem_bytes(cfg->dtype), e, cfg->select_mode == CITRUS_SELECT_PER_LAYER, make_view(k_new),
-                                      make_view(v_new), make_view(k_cache), make_view(v_cache), st));
+  return hip_status(launch_decode_evict(cfg->dtype, a, e, cfg->select_mode == CITRUS_SELECT_PER_LAYER, static_cast<hipStream_t>(hip_stream)));
 }
 
 int32_t citrus_score_accumulate(const citrus_config* cfg, float* score, int32_t n, const float* acc,

@@ -138,7 +138,8 @@ size_t decode_mfma_workspace_floats(const Dims& dm);
 hipError_t launch_decode_mfma(const Dims& dm, View q, Segments kseg, Segments vseg, View out, float* workspace,
                               int append_token, hipStream_t st);
 
-// ---- generation: a few query rows per head over a cache and ks.c <= 64 states of their own, tree_attn.hip ----
+// ---- generation: a few query rows per head over a cache and ks.c <= 64 states of their own ----
+// Launches and the commit of a path: tree_attn.hip
 constexpr int kMaxNodes = 64;
 struct FewRows {
   Dims dm;
@@ -148,16 +149,45 @@ struct FewRows {
   const uint64_t* words;  // optional: bit u of words[b * words_sb + t] says that row t sees state u of its own
   int64_t words_sb;
   View out;
-  float* lse;             // optional [B, L, Hq, c]: natural logarithm ...
-  float* lse2;            // ... and base 2
-  float* scores;          // optional [B, L, Hq][score_pitch] (c == 1): the logits, base 2
-  int64_t score_pitch;
+  float* lse;             // optional [B, L, Hq, c]
+  float* scores;          // a token's logits, base 2: [B, L, Hq][score_pitch]
+  int64_t score_pitch;    // a multiple of 32
   float* workspace;       // few_rows_workspace_floats
+  // of the launch: ranges of keys, and where their parts of the rows go (NULL: there is one, and it finishes its rows)
+  int splits;
+  float2* part_ml;        // [range][B*L*Hq*c]: maximum (base 2), sum
+  float* part_o;          // [range][B*L*Hq*c][D]
 };
 size_t few_rows_workspace_floats(int dtype, const Dims& dm, int rows);  // for any call with at most `rows` rows per head
-hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t st);
-size_t few_rows_bf16_workspace_floats(const Dims& dm, int rows);  // few_rows_bf16.hip
-hipError_t launch_few_rows_bf16(const FewRows& a, hipStream_t st);
+hipError_t launch_tree_attn(int dtype, FewRows a, hipStream_t st);
+
+// The states' sums of attention weights and the state that makes room for the token's.
+struct EvictStep {
+  Dims dm;
+  int n;                 // cached states
+  int start, recent;     // the slots that are kept, at the front and at the end, ...
+  int oldest;            // ... but for this one of the latter; -1: the cache grows
+  float* acc;            // [B, L, Hkv][acc_pitch]
+  int64_t acc_pitch;
+  View k_new, v_new, k_cache, v_cache;
+  int row_bytes;
+  int32_t* evicted;      // optional [B, L, Hsel]
+  float* own;            // scratch [B, L, Hkv]: the token's weight
+  float2* best;          // scratch [B, L, Hkv][evict_step_ranges]
+};
+int evict_step_ranges(int n);
+hipError_t launch_decode_evict(int dtype, FewRows a, const EvictStep& ev, bool per_layer, hipStream_t st);
+
+// Their parts.  The attention in rows and keys, few_rows_bf16.hip and few_rows_f32.hip; ev: logits are kept, and p.evicts: acted upon.
+struct FewRowsPlan {
+  int waves, kh;         // of a workgroup; waves that share the keys of a block of 32 rows
+  int row_groups, splits;
+  bool evicts;
+};
+hipError_t launch_few_rows_bf16(const FewRows& a, const FewRowsPlan& p, const EvictStep* ev, hipStream_t st);
+hipError_t launch_few_rows_f32(const FewRows& a, const FewRowsPlan& p, const EvictStep* ev, hipStream_t st);
+// The eviction behind it, evict_step.hip.
+hipError_t launch_evict_step(int dtype, const FewRows& a, const EvictStep& ev, bool per_layer, hipStream_t st);
 
 struct Commit {
   const int32_t *path, *accepted, *lens;  // [B][path_len], [B], optional [B]
@@ -166,25 +196,6 @@ struct Commit {
 };
 hipError_t launch_tree_commit(int elem_bytes, const Dims& dm, View k_draft, View v_draft, View k_cache, View v_cache,
                               const Commit& a, hipStream_t st);
-
-// ---- generation: the states' sums of attention weights and the state that makes room, evict_step.hip ----
-struct EvictStep {
-  Dims dm;
-  int n;                 // cached states
-  int start, recent;     // the slots that are kept, at the front and at the end, ...
-  int oldest;            // ... but for this one of the latter; -1: the cache grows
-  float* acc;            // [B, L, Hkv][acc_pitch]
-  int64_t acc_pitch;
-  const float* scores;   // [B, L, Hq][score_pitch], base 2, the token's own behind the n states'
-  int64_t score_pitch;
-  const float* lse2;     // [B, L, Hq]
-  float* own;            // [B, L, Hkv]: the token's weight
-  float2* best;          // [B, L, Hkv][ranges of keys]
-  int32_t* evicted;      // optional [B, L, Hsel]
-};
-int evict_step_ranges(int n);
-hipError_t launch_evict_step(int elem_bytes, const EvictStep& a, bool per_layer, View k_new, View v_new, View k_cache,
-                             View v_cache, hipStream_t st);
 
 // ---- rotary embedding at explicit positions, rope.hip ----
 // y[b,l,h,s,:] = RoPE(x[b,l,h,s,:], pos0 + s) for h < heads, s < rows; y may be x itself.

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "bf16_math.h"
 #include "citrus_internal.h"
 
 namespace citrus {
@@ -18,26 +19,81 @@ __device__ inline const E* row_ptr(const View& v, int b, int l, int h, int64_t r
   return static_cast<const E*>(v.ptr) + (b * v.sb + l * v.sl + h * v.sh + row * v.ss);
 }
 
-// Elements of a 16-byte piece of a row as f32 numbers: eight bf16 words or four floats.
-template <typename E>
-struct Piece {
-  static constexpr int kN = 16 / sizeof(E);
-  float x[kN];
-};
-__device__ inline Piece<uint16_t> load_piece(const uint16_t* p) {
-  const uint4 v = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  Piece<uint16_t> f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f.x[2 * i] = __uint_as_float(w[i] << 16);
-    f.x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-  return f;
+__device__ inline void store4(uint16_t* p, const float (&o)[4]) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
 }
-__device__ inline Piece<float> load_piece(const float* p) {
-  const float4 v = *reinterpret_cast<const float4*>(p);
-  return Piece<float>{{v.x, v.y, v.z, v.w}};
+__device__ inline void store4(float* p, const float (&o)[4]) { *reinterpret_cast<float4*>(p) = make_float4(o[0], o[1], o[2], o[3]); }
+
+// Parts of a row over different keys become one: what each holds of it is {maximum (base 2), sum} and four elements before the division.
+struct RowParts {
+  float m = -INFINITY, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  __device__ float reference() const { return m == -INFINITY ? 0.f : m; }  // nothing seen: every weight is 0
+  __device__ void add(const float2& ml, const float4& x) {
+    const float w = __builtin_amdgcn_exp2f(ml.x - reference());
+    sum = fmaf(ml.y, w, sum);
+    o[0] = fmaf(x.x, w, o[0]);
+    o[1] = fmaf(x.y, w, o[1]);
+    o[2] = fmaf(x.z, w, o[2]);
+    o[3] = fmaf(x.w, w, o[3]);
+  }
+};
+
+// Four elements of a row's result, and with the first of them its log-sum-exp.
+template <typename E>
+__device__ inline void finish_row(const FewRows& a, int b, int l, int h, int t, int64_t row, int d, RowParts& r, float* lse2 = nullptr) {
+  const bool real = a.words == nullptr || (a.words[b * a.words_sb + t] >> t & 1);
+#pragma unroll
+  for (int x = 0; x < 4; ++x) r.o[x] = real ? r.o[x] / r.sum : 0.f;
+  store4(const_cast<E*>(row_ptr<E>(a.out, b, l, h, t)) + d, r.o);
+  if (d == 0) {
+    const float v = real ? r.reference() + log2f(r.sum) : -INFINITY;
+    if (a.lse != nullptr) a.lse[row] = v * kLn2;
+    if (lse2 != nullptr) *lse2 = v;
+  }
+}
+
+// The waves of a workgroup have left their parts in LDS, o_s[wave][32 rows][D + 4] and ml_s[wave][32]; KH of them share a block of 32 rows.
+// The workgroup's `here` rows from `first` on of KV head g; lse2 (optional, LDS): base 2, by row of this workgroup.
+template <typename E, int D, int WAVES, int KH>
+__device__ __forceinline__ void join_waves(const FewRows& a, const float* o_s, const float2* ml_s, int g, int first, int here, int sp,
+                                           float* lse2 = nullptr) {
+  constexpr int kPitch = D + 4;
+  const Dims& dm = a.dm;
+  const int nodes = a.ks.c, b = blockIdx.y / dm.L, l = blockIdx.y % dm.L;
+  for (int e = threadIdx.x; e < here * (D / 4); e += 64 * WAVES) {
+    const int r = e / (D / 4), d = e % (D / 4) * 4;
+    const int at = (r / 32 * KH) * 32 + r % 32;
+    RowParts p;
+#pragma unroll
+    for (int w = 0; w < KH; ++w) p.m = fmaxf(p.m, ml_s[at + 32 * w].x);
+#pragma unroll
+    for (int w = 0; w < KH; ++w) p.add(ml_s[at + 32 * w], *reinterpret_cast<const float4*>(o_s + (at + 32 * w) * kPitch + d));
+    const int h = g * dm.G + (first + r) / nodes, t = (first + r) % nodes;
+    const int64_t row = (static_cast<int64_t>(blockIdx.y) * dm.Hq + h) * nodes + t;
+    if (a.part_o == nullptr) {
+      finish_row<E>(a, b, l, h, t, row, d, p, lse2 != nullptr ? lse2 + r : nullptr);
+    } else {
+      const int64_t at_part = static_cast<int64_t>(sp) * dm.B * dm.L * dm.Hq * nodes + row;
+      *reinterpret_cast<float4*>(a.part_o + at_part * D + d) = make_float4(p.o[0], p.o[1], p.o[2], p.o[3]);
+      if (d == 0) a.part_ml[at_part] = make_float2(p.m, p.sum);
+    }
+  }
+}
+
+// Four elements of a row from its ranges of keys.
+template <int D>
+__device__ inline RowParts join_ranges(const FewRows& a, int64_t row, int d) {
+  const int64_t all = static_cast<int64_t>(a.dm.B) * a.dm.L * a.dm.Hq * a.ks.c;
+  RowParts p;
+  for (int s = 0; s < a.splits; ++s) p.m = fmaxf(p.m, a.part_ml[s * all + row].x);
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s) p.add(a.part_ml[s * all + row], *reinterpret_cast<const float4*>(a.part_o + (s * all + row) * D + d));
+  return p;
+}
+
+// What a lane sees of the 32 keys from own + n_c on: bit j, by its node's word.
+__device__ inline uint32_t seen_keys(uint64_t word, int own) {
+  return own >= 0 ? static_cast<uint32_t>(word >> own) : static_cast<uint32_t>(word) << -own | ((1u << -own) - 1);
 }
 
 }  // namespace

@@ -7,7 +7,8 @@
 //   PRIVATE  up to 32 rows: every wave streams 32-key tiles of its own through LDS, with no barrier between the waves;
 //   shared   more rows: the waves of a workgroup read the same 64-key stages, four of them in LDS, a block of 32 rows per KH waves
 //            (KH = 2: each takes half of a stage's keys), one barrier a stage.
-// Keys are split over workgroups where the units do not fill the chip, and few_rows_merge_kernel joins the ranges.
+// Keys are split over workgroups where the units do not fill the chip; another launch joins the ranges.
+#include "evict_unit.h"
 #include "key_stream.h"
 
 namespace citrus {
@@ -17,13 +18,7 @@ typedef __attribute__((address_space(3))) void* lds_void_ptr;
 typedef __attribute__((address_space(3))) char* lds_char_ptr;
 
 constexpr int kStageKeys = 64, kStages = 4;  // shared form
-constexpr int kMostSplits = 64;
-
-// Results of a range of keys: {maximum (base 2), sum} and the row before its division.
-struct Partials {
-  float2* ml;  // [range][B*L*Hq*T]
-  float* o;    // [range][B*L*Hq*T][D]
-};
+constexpr int kLdsOfUnit = 160 * 1024, kLdsOfVote = 1024;  // __syncthreads_and has some of its own, in front of the tiles
 
 // What the lanes of one query row hold of it.
 template <int D>
@@ -40,22 +35,6 @@ __device__ inline float zero_if_finite(const Pack8& a, float sum) {
   return sum;
 }
 
-// Four elements of a row's result.  m: the maximum its sum was formed with.
-__device__ inline void finish_row(const FewRows& a, int b, int l, int h, int t, int64_t row, int d, float m, float sum, const float (&o)[4]) {
-  const bool real = a.words == nullptr || (a.words[b * a.words_sb + t] >> t & 1);
-  uint2 w = {0, 0};
-  if (real) {
-    w.x = pack_bf16x2(o[0] / sum, o[1] / sum);
-    w.y = pack_bf16x2(o[2] / sum, o[3] / sum);
-  }
-  *reinterpret_cast<uint2*>(const_cast<uint16_t*>(row_ptr<uint16_t>(a.out, b, l, h, t)) + d) = w;
-  if (d == 0) {
-    const float lse2 = real ? m + log2f(sum) : -INFINITY;
-    if (a.lse != nullptr) a.lse[row] = lse2 * kLn2;
-    if (a.lse2 != nullptr) a.lse2[row] = lse2;
-  }
-}
-
 // vmcnt(LEFT), nothing else
 template <int LEFT>
 __device__ inline void wait_loads() {
@@ -65,8 +44,8 @@ __device__ inline void wait_loads() {
 }
 
 // One 32-key tile.  LAST: keys that not every row sees; bit j of `seen` says that this lane's row sees key j of the tile.
-// PARTS: bf16 words of a weight in P.V.
-template <int D, int PARTS, bool LAST>
+// PARTS: bf16 words of a weight in P.V.  CAREFUL: see few_rows_kernel.
+template <int D, int PARTS, bool LAST, bool CAREFUL>
 __device__ __forceinline__ void key_tile(uint32_t k_t, uint32_t v_t, const uint32_t (&k_off)[Geo<D>::kKk], const uint32_t (&v_off)[2 * Geo<D>::kOut],
                                          const bf16x8 (&q_op)[Geo<D>::kKk], float c2, uint32_t seen, Column<D>& c, float* scores) {
   typedef Geo<D> T;
@@ -132,10 +111,9 @@ __device__ __forceinline__ void key_tile(uint32_t k_t, uint32_t v_t, const uint3
       for (int e = 0; e < 2 * T::kOut; ++e) addr[e] = v_t + 16 * half * T::kRowBytes + v_off[e];
       lds_read_v_operands(av, addr);
     }
-    if constexpr (LAST || PARTS == 2) {
-      // 0 x infinity is NaN: a value that some row does not see, or the second part of a weight that one part holds.  Values that
-      // are infinite or NaN are taken out of the operands and their products added one by one, to the rows that see them: what
-      // a row does not see leaves the bits of its result alone.
+    if constexpr (CAREFUL) {
+      // Values that are infinite or NaN are taken out of the operands and their products added one by one, to the rows that see
+      // them: the other rows get the bits that any finite values would give.
       float zero = 0.f;
 #pragma unroll
       for (int r = 0; r < T::kOut; ++r) zero = zero_if_finite(av[r], zero);
@@ -185,9 +163,25 @@ __device__ __forceinline__ void key_tile(uint32_t k_t, uint32_t v_t, const uint3
   }
 }
 
+// A matrix product forms 0 x v too, for values that a row does not see, and p_lo x v for the second part of a weight whose first part
+// said it all: an infinite or NaN value then leaves NaN in rows that must be finite, or infinite.  Nothing in the loop looks for such
+// values; a workgroup whose results are not all finite goes over its keys once more, carefully.
+//
 // grid: (row groups * Hkv * key ranges, B * L)
-template <int D, int WAVES, int KH, int PARTS, bool SCORES>
-__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, int key_splits, Partials part) {
+template <int D, int WAVES, int KH>
+struct Lds {
+  static constexpr int kRows = WAVES * 32 * (D + 4) * 4, kJoin = kRows + WAVES * 32 * 8;  // o_s, ml_s
+  static constexpr int kAfter = kJoin + 32 * 4 + (WAVES + 1) * 8;                         // lse2, Candidates
+  static constexpr int kTiles = KH == WAVES ? WAVES * Geo<D>::kWaveLdsBytes : kStages * (kStageKeys / 32) * 2 * Geo<D>::kTileBytes;
+  static constexpr int kBytes = ((kAfter > kTiles ? kAfter : kTiles) + 15) / 16 * 16;  // ... the strip of logits
+};
+// A unit's logits in LDS: the pitch of a head.  Heads four words apart from the same bank.
+__host__ __device__ inline int strip_pitch(int n) { return (n + 1 + 31) / 32 * 32 + 4; }
+
+// Where a single token's logits go: to the workspace, for other kernels; or the unit is one workgroup's, which evicts by them.
+enum class Logits { kNone, kKept, kEvict, kEvictInLds };
+template <int D, int WAVES, int KH, int PARTS, Logits LOGITS>
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictStep ev) {
   typedef Geo<D> T;
   constexpr bool kPrivate = KH == WAVES;
   constexpr int kBlocks = WAVES / KH;  // of 32 rows
@@ -196,6 +190,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, int key
   const Dims& dm = a.dm;
   const int lane = threadIdx.x % 64, col = lane % 32, grp = lane / 32;
   const int wu = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int key_splits = a.splits;
   const int sp = blockIdx.x % key_splits, g = blockIdx.x / key_splits % dm.Hkv, row_group = blockIdx.x / key_splits / dm.Hkv;
   const int b = blockIdx.y / dm.L, l = blockIdx.y % dm.L;
   const int nodes = a.ks.c, rows = dm.G * nodes;
@@ -269,86 +264,97 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, int key
 
   const float c2 = dm.scale * kLog2e;
   Column<D> c;
+  float* scores = nullptr;  // of this lane's row
+  if constexpr (LOGITS == Logits::kEvictInLds) {
+    if (row < rows) scores = reinterpret_cast<float*>(lds + Lds<D, WAVES, KH>::kBytes) + row * strip_pitch(ev.n);
+  } else if constexpr (LOGITS != Logits::kNone) {
+    if (row < rows) scores = a.scores + (static_cast<int64_t>(blockIdx.y) * dm.Hq + h) * a.score_pitch;
+  }
+
+  auto over_the_keys = [&]<bool CAREFUL>() {
+    c.m = -INFINITY;
+    c.l = 0.f;
+#pragma unroll
+    for (int r = 0; r < T::kOut; ++r)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) c.o[r][i] = 0.f;
+    auto tile = [&](int j0, uint32_t k_t, uint32_t v_t) {
+      float* const s = LOGITS != Logits::kNone && scores != nullptr ? scores + j0 : nullptr;
+      const int own = j0 - n_c;  // of the tile's first key
+      if (own + 32 <= 0) {
+        key_tile<D, PARTS, false, CAREFUL>(k_t, v_t, k_off, v_off, q_op, c2, 0, c, s);
+      } else {
+        key_tile<D, PARTS, true, CAREFUL>(k_t, v_t, k_off, v_off, q_op, c2, seen_keys(word, own), c, s);
+      }
+    };
+    if constexpr (kPrivate) {
+      // key tiles of this workgroup's range, dealt to its waves in turn
+      const int tiles = (n + 31) / 32, per = (tiles + key_splits - 1) / key_splits;
+      const int end = min(tiles, (sp + 1) * per);
+      char* const mine = lds + wu * T::kWaveLdsBytes;  // [buffer][K | V][tile]
+      const uint32_t mine_at = lds_at + wu * T::kWaveLdsBytes;
+      auto fill_tile = [&](int x, int buf) {
+        char* k_t = mine + buf * 2 * kTileBytes;
+        fill(x * 32, 0, 32 / kR, k_t, k_t + kTileBytes);
+      };
+      int x = sp * per + wu;
+      if (x < end) fill_tile(x, 0);
+      for (int it = 0; x < end; x += WAVES, ++it) {
+        const int buf = it & 1;
+        // the other buffer was last read in the previous turn, whose reads have all returned
+        if (x + WAVES < end) {
+          fill_tile(x + WAVES, buf ^ 1);
+          wait_loads<T::kLoadsPerTile>();
+        } else {
+          wait_loads<0>();
+        }
+        const uint32_t k_t = mine_at + buf * 2 * kTileBytes;
+        tile(x * 32, k_t, k_t + kTileBytes);
+      }
+    } else {
+      constexpr int kSub = kStageKeys / 32, kStageBytes = 2 * kSub * kTileBytes, kGroups = kStageKeys / kR / WAVES;
+      constexpr int kLoads = 2 * kGroups;  // of a wave and stage, at least (the stage behind the cache's last row takes more)
+      static_assert(kGroups >= 1 && kSub % KH == 0);
+      const int stages = (n + kStageKeys - 1) / kStageKeys, per = (stages + key_splits - 1) / key_splits;
+      const int begin = sp * per, end = min(stages, begin + per);
+      auto fill_stage = [&](int x) {
+        char* k_t = lds + (x - begin) % kStages * kStageBytes;
+        fill(x * kStageKeys, wu * kGroups, kGroups, k_t, k_t + kSub * kTileBytes);
+      };
+      for (int x = begin; x < min(end, begin + kStages - 1); ++x) fill_stage(x);
+      for (int x = begin; x < end; ++x) {
+        // this wave's loads of the stage have landed; behind the barrier everybody's have, and the stage before has been read
+        if (x + kStages - 2 < end)
+          wait_loads<kLoads*(kStages - 2)>();
+        else
+          wait_loads<0>();
+        asm volatile("s_barrier" ::: "memory");
+        if (x + kStages - 1 < end) fill_stage(x + kStages - 1);
+        if (idle) continue;
+        const uint32_t k_t = lds_at + (x - begin) % kStages * kStageBytes, v_t = k_t + kSub * kTileBytes;
+#pragma unroll
+        for (int y = 0; y < kSub / KH; ++y) {
+          const int sub = KH == 1 ? y : wu % KH;
+          const int j0 = x * kStageKeys + 32 * sub;
+          if (j0 < n) tile(j0, k_t + sub * kTileBytes, v_t + sub * kTileBytes);
+        }
+      }
+    }
+  };
+  over_the_keys.template operator()<false>();
+  bool finite = true;
 #pragma unroll
   for (int r = 0; r < T::kOut; ++r)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) c.o[r][i] = 0.f;
-  float* scores = nullptr;
-  if constexpr (SCORES)
-    if (row < rows) scores = a.scores + (static_cast<int64_t>(blockIdx.y) * dm.Hq + h) * a.score_pitch;
-
-  auto tile = [&](int j0, uint32_t k_t, uint32_t v_t) {
-    float* const s = SCORES && scores != nullptr ? scores + j0 : nullptr;
-    const int own = j0 - n_c;  // of the tile's first key
-    if (own + 32 <= 0) {
-      key_tile<D, PARTS, false>(k_t, v_t, k_off, v_off, q_op, c2, 0, c, s);
-    } else {
-      const uint32_t seen = own >= 0 ? static_cast<uint32_t>(word >> own)
-                                     : static_cast<uint32_t>(word) << -own | ((1u << -own) - 1);
-      key_tile<D, PARTS, true>(k_t, v_t, k_off, v_off, q_op, c2, seen, c, s);
-    }
-  };
-
-  if constexpr (kPrivate) {
-    // key tiles of this workgroup's range, dealt to its waves in turn
-    const int tiles = (n + 31) / 32, per = (tiles + key_splits - 1) / key_splits;
-    const int end = min(tiles, (sp + 1) * per);
-    char* const mine = lds + wu * T::kWaveLdsBytes;  // [buffer][K | V][tile]
-    const uint32_t mine_at = lds_at + wu * T::kWaveLdsBytes;
-    auto fill_tile = [&](int x, int buf) {
-      char* k_t = mine + buf * 2 * kTileBytes;
-      fill(x * 32, 0, 32 / kR, k_t, k_t + kTileBytes);
-    };
-    int x = sp * per + wu;
-    if (x < end) fill_tile(x, 0);
-    for (int it = 0; x < end; x += WAVES, ++it) {
-      const int buf = it & 1;
-      // the other buffer was last read in the previous turn, whose reads have all returned
-      if (x + WAVES < end) {
-        fill_tile(x + WAVES, buf ^ 1);
-        wait_loads<T::kLoadsPerTile>();
-      } else {
-        wait_loads<0>();
-      }
-      const uint32_t k_t = mine_at + buf * 2 * kTileBytes;
-      tile(x * 32, k_t, k_t + kTileBytes);
-    }
-  } else {
-    constexpr int kSub = kStageKeys / 32, kStageBytes = 2 * kSub * kTileBytes, kGroups = kStageKeys / kR / WAVES;
-    constexpr int kLoads = 2 * kGroups;  // of a wave and stage, at least (the stage behind the cache's last row takes more)
-    static_assert(kGroups >= 1 && kSub % KH == 0);
-    const int stages = (n + kStageKeys - 1) / kStageKeys, per = (stages + key_splits - 1) / key_splits;
-    const int begin = sp * per, end = min(stages, begin + per);
-    auto fill_stage = [&](int x) {
-      char* k_t = lds + (x - begin) % kStages * kStageBytes;
-      fill(x * kStageKeys, wu * kGroups, kGroups, k_t, k_t + kSub * kTileBytes);
-    };
-    for (int x = begin; x < min(end, begin + kStages - 1); ++x) fill_stage(x);
-    for (int x = begin; x < end; ++x) {
-      // this wave's loads of the stage have landed; behind the barrier everybody's have, and the stage before has been read
-      if (x + kStages - 2 < end)
-        wait_loads<kLoads*(kStages - 2)>();
-      else
-        wait_loads<0>();
-      asm volatile("s_barrier" ::: "memory");
-      if (x + kStages - 1 < end) fill_stage(x + kStages - 1);
-      if (idle) continue;
-      const uint32_t k_t = lds_at + (x - begin) % kStages * kStageBytes, v_t = k_t + kSub * kTileBytes;
-#pragma unroll
-      for (int y = 0; y < kSub / KH; ++y) {
-        const int sub = KH == 1 ? y : wu % KH;
-        const int j0 = x * kStageKeys + 32 * sub;
-        if (j0 < n) tile(j0, k_t + sub * kTileBytes, v_t + sub * kTileBytes);
-      }
-    }
-  }
+    for (int i = 0; i < 16; ++i) finite &= fabsf(c.o[r][i]) < INFINITY;
+  if (!__syncthreads_and(finite || row >= rows || !(word >> t & 1))) over_the_keys.template operator()<true>();
 
   // ---- the waves of a block of rows join through LDS (the tiles have been read when every wave is here) ----
   constexpr int kPitch = D + 4;
   const float l_row = c.l + __shfl_xor(c.l, 32, 64);
   __syncthreads();
   float* const o_s = reinterpret_cast<float*>(lds);                                       // [wave][32 rows][kPitch]
-  float2* const ml_s = reinterpret_cast<float2*>(lds + WAVES * 32 * kPitch * sizeof(float));  // [wave][32]
+  float2* const ml_s = reinterpret_cast<float2*>(lds + Lds<D, WAVES, KH>::kRows);  // [wave][32]
   if (row < rows) {
     if (grp == 0) ml_s[wu * 32 + col] = make_float2(c.m, l_row);
 #pragma unroll
@@ -363,139 +369,53 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, int key
   }
   __syncthreads();
   const int first = row_group * kBlocks * 32, here = min(kBlocks * 32, rows - first);
-  for (int e = threadIdx.x; e < here * (D / 4); e += 64 * WAVES) {
-    const int r = e / (D / 4), d = e % (D / 4) * 4;
-    const int at = (r / 32 * KH) * 32 + r % 32;
-    float m = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < KH; ++w) m = fmaxf(m, ml_s[at + 32 * w].x);
-    const float m_use = m == -INFINITY ? 0.f : m;
-    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < KH; ++w) {
-      const float2 ml = ml_s[at + 32 * w];
-      const float wgt = __builtin_amdgcn_exp2f(ml.x - m_use);
-      const float4 x = *reinterpret_cast<const float4*>(o_s + (at + 32 * w) * kPitch + d);
-      sum = fmaf(ml.y, wgt, sum);
-      o[0] = fmaf(x.x, wgt, o[0]);
-      o[1] = fmaf(x.y, wgt, o[1]);
-      o[2] = fmaf(x.z, wgt, o[2]);
-      o[3] = fmaf(x.w, wgt, o[3]);
-    }
-    const int hq = g * dm.G + (first + r) / nodes, tt = (first + r) % nodes;
-    const int64_t at_row = (static_cast<int64_t>(blockIdx.y) * dm.Hq + hq) * nodes + tt;
-    if (key_splits == 1) {
-      finish_row(a, b, l, hq, tt, at_row, d, m_use, sum, o);
-    } else {
-      const int64_t p = static_cast<int64_t>(sp) * dm.B * dm.L * dm.Hq * nodes + at_row;
-      *reinterpret_cast<float4*>(part.o + p * D + d) = make_float4(o[0], o[1], o[2], o[3]);
-      if (d == 0) part.ml[p] = make_float2(m, sum);
-    }
+  if constexpr (LOGITS == Logits::kNone || LOGITS == Logits::kKept) {
+    join_waves<uint16_t, D, WAVES, KH>(a, o_s, ml_s, g, first, here, sp);
+  } else {
+    float* const lse2 = reinterpret_cast<float*>(lds + Lds<D, WAVES, KH>::kJoin);
+    join_waves<uint16_t, D, WAVES, KH>(a, o_s, ml_s, g, first, here, sp, lse2);
+    __syncthreads();
+    Candidate* const scratch = reinterpret_cast<Candidate*>(lse2 + 32);
+    if constexpr (LOGITS == Logits::kEvictInLds)
+      evict_unit<64 * WAVES>(ev, b, l, g, reinterpret_cast<const float*>(lds + Lds<D, WAVES, KH>::kBytes), strip_pitch(ev.n), lse2, scratch);
+    else
+      evict_unit<64 * WAVES>(ev, b, l, g, a.scores + (static_cast<int64_t>(blockIdx.y) * dm.Hq + g * dm.G) * a.score_pitch, a.score_pitch,
+                             lse2, scratch);
   }
 }
 
-// The ranges of keys join: one thread per four elements of a row.
-template <int D>
-__global__ __launch_bounds__(256) void few_rows_merge_kernel(FewRows a, int key_splits, Partials part) {
-  const Dims& dm = a.dm;
-  const int nodes = a.ks.c;
-  const int e = blockIdx.x * 256 + threadIdx.x;
-  if (e >= dm.Hq * nodes * (D / 4)) return;
-  const int d = e % (D / 4) * 4, r = e / (D / 4);
-  const int64_t all = static_cast<int64_t>(dm.B) * dm.L * dm.Hq * nodes, row = static_cast<int64_t>(blockIdx.y) * dm.Hq * nodes + r;
-  float m = -INFINITY;
-  for (int s = 0; s < key_splits; ++s) m = fmaxf(m, part.ml[s * all + row].x);
-  const float m_use = m == -INFINITY ? 0.f : m;
-  float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < key_splits; ++s) {
-    const float2 ml = part.ml[s * all + row];
-    const float wgt = __builtin_amdgcn_exp2f(ml.x - m_use);
-    const float4 x = *reinterpret_cast<const float4*>(part.o + (s * all + row) * D + d);
-    sum = fmaf(ml.y, wgt, sum);
-    o[0] = fmaf(x.x, wgt, o[0]);
-    o[1] = fmaf(x.y, wgt, o[1]);
-    o[2] = fmaf(x.z, wgt, o[2]);
-    o[3] = fmaf(x.w, wgt, o[3]);
-  }
-  finish_row(a, blockIdx.y / dm.L, blockIdx.y % dm.L, r / nodes, r % nodes, row, d, m_use, sum, o);
-}
-
-// How a call is launched.
-struct Plan {
-  int waves, kh, row_groups, splits;
-};
-// Ranges of keys.  A compute unit holds one workgroup (head_dim 64: two); rounds of the chip times a workgroup's share of the
-// keys is what the launch takes, and a second launch costs about as much as eight 32-key tiles of a workgroup's stream.
-Plan plan_for(const Dims& dm, int nodes, int most_keys, bool scores) {
-  const int blocks = (dm.G * nodes + 31) / 32;
-  Plan p;
-  p.waves = blocks <= 2 || scores ? 4 : 8;
-  p.kh = blocks == 1 || scores ? 4 : blocks <= 4 ? 2 : 1;
-  p.row_groups = (blocks + p.waves / p.kh - 1) / (p.waves / p.kh);
-  const int64_t groups = static_cast<int64_t>(dm.B) * dm.L * dm.Hkv * p.row_groups, slots = dm.D == 128 ? 256 : 512;
-  const int unit = p.kh == 4 ? 32 : kStageKeys, tiles = (most_keys + unit - 1) / unit;
-  int64_t best = INT64_MAX;
-  p.splits = 1;
-  for (int s = 1; s <= kMostSplits && s * groups <= 4 * slots; ++s) {
-    const int per = (tiles + s - 1) / s;
-    if (s > 1 && per * unit < 128) break;
-    if ((tiles + per - 1) / per != s) continue;  // no empty ranges
-    const int64_t cost = (s * groups + slots - 1) / slots * (per * unit / 32 + 6) + (s > 1 ? 8 : 0);
-    if (cost < best) best = cost, p.splits = s;
-  }
-  return p;
-}
-size_t partial_floats(const Dims& dm, int nodes, int splits) {
-  return splits == 1 ? 0 : static_cast<size_t>(splits) * dm.B * dm.L * dm.Hq * nodes * (dm.D + 2);
-}
-
-template <int D, int WAVES, int KH, int PARTS, bool SCORES>
-hipError_t launch(const FewRows& a, const Plan& p, const Partials& part, hipStream_t st) {
-  constexpr int kJoin = WAVES * 32 * ((D + 4) * 4 + 8);
-  constexpr int kTiles = KH == WAVES ? WAVES * Geo<D>::kWaveLdsBytes : kStages * (kStageKeys / 32) * 2 * Geo<D>::kTileBytes;
-  constexpr int kLds = kJoin > kTiles ? kJoin : kTiles;
+template <int D, int WAVES, int KH, int PARTS, Logits LOGITS>
+hipError_t launch(const FewRows& a, const EvictStep& ev, int row_groups, hipStream_t st) {
+  typedef Lds<D, WAVES, KH> L;
+  const int strip = LOGITS == Logits::kEvictInLds ? a.dm.G * strip_pitch(ev.n) * 4 : 0;
   static LdsLimit limit;
-  const auto kernel = few_rows_kernel<D, WAVES, KH, PARTS, SCORES>;
-  hipError_t e = raise_lds_limit(limit, reinterpret_cast<const void*>(kernel), kLds);
+  const auto kernel = few_rows_kernel<D, WAVES, KH, PARTS, LOGITS>;
+  const hipError_t e = raise_lds_limit(limit, reinterpret_cast<const void*>(kernel), LOGITS == Logits::kEvictInLds ? kLdsOfUnit - kLdsOfVote : L::kBytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(p.row_groups * a.dm.Hkv * p.splits, a.dm.B * a.dm.L), dim3(64 * WAVES), kLds, st, a, p.splits, part);
+  hipLaunchKernelGGL(kernel, dim3(row_groups * a.dm.Hkv * a.splits, a.dm.B * a.dm.L), dim3(64 * WAVES), L::kBytes + strip, st, a, ev);
   return hipGetLastError();
 }
 template <int D>
-hipError_t launch_all(const FewRows& a, hipStream_t st) {
-  const Plan p = plan_for(a.dm, a.ks.c, a.ks.n_c + a.ks.c, a.scores != nullptr);
-  Partials part{nullptr, nullptr};
-  if (p.splits > 1) {
-    part.o = a.workspace;
-    part.ml = reinterpret_cast<float2*>(a.workspace + static_cast<size_t>(p.splits) * a.dm.B * a.dm.L * a.dm.Hq * a.ks.c * D);
+hipError_t launch_form(const FewRows& a, const FewRowsPlan& p, const EvictStep* ev, hipStream_t st) {
+  const EvictStep none{};
+  if (ev != nullptr) {
+    // the strip lies in LDS where that leaves as many workgroups to a compute unit as there are without it
+    const int units = D == 128 ? 1 : 2;
+    const bool fits = a.dm.G * strip_pitch(ev->n) * 4 + Lds<D, 4, 4>::kBytes <= kLdsOfUnit / units - kLdsOfVote;
+    return !p.evicts ? launch<D, 4, 4, 2, Logits::kKept>(a, none, p.row_groups, st)
+           : fits    ? launch<D, 4, 4, 2, Logits::kEvictInLds>(a, *ev, p.row_groups, st)
+                     : launch<D, 4, 4, 2, Logits::kEvict>(a, *ev, p.row_groups, st);
   }
-  hipError_t e = a.scores != nullptr ? launch<D, 4, 4, 2, true>(a, p, part, st)
-                 : p.kh == 4         ? launch<D, 4, 4, 2, false>(a, p, part, st)
-                 : p.waves == 4      ? launch<D, 4, 2, 2, false>(a, p, part, st)
-                 : p.kh == 2         ? launch<D, 8, 2, 2, false>(a, p, part, st)
-                                     : launch<D, 8, 1, D == 64 ? 2 : 1, false>(a, p, part, st);
-  if (e != hipSuccess || p.splits == 1) return e;
-  const int pieces = a.dm.Hq * a.ks.c * (D / 4);
-  hipLaunchKernelGGL(few_rows_merge_kernel<D>, dim3((pieces + 255) / 256, a.dm.B * a.dm.L), dim3(256), 0, st, a, p.splits, part);
-  return hipGetLastError();
+  return p.kh == 4      ? launch<D, 4, 4, 2, Logits::kNone>(a, none, p.row_groups, st)
+         : p.waves == 4 ? launch<D, 4, 2, 2, Logits::kNone>(a, none, p.row_groups, st)
+         : p.kh == 2    ? launch<D, 8, 2, 2, Logits::kNone>(a, none, p.row_groups, st)
+                        : launch<D, 8, 1, D == 64 ? 2 : 1, Logits::kNone>(a, none, p.row_groups, st);
 }
 
 }  // namespace
 
-size_t few_rows_bf16_workspace_floats(const Dims& dm, int rows) {
-  size_t most = 0;
-  for (int t = 1; t <= rows; ++t)
-    for (int scores = 0; scores < (t == 1 ? 2 : 1); ++scores) {
-      const int blocks = (dm.G * t + 31) / 32, kh = blocks == 1 || scores ? 4 : blocks <= 4 ? 2 : 1;
-      const int per = (blocks <= 2 || scores ? 4 : 8) / kh;
-      const int64_t groups = static_cast<int64_t>(dm.B) * dm.L * dm.Hkv * ((blocks + per - 1) / per), slots = dm.D == 128 ? 256 : 512;
-      const int64_t s = 4 * slots / groups;
-      const size_t f = partial_floats(dm, t, static_cast<int>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s));
-      if (f > most) most = f;
-    }
-  return most;
+hipError_t launch_few_rows_bf16(const FewRows& a, const FewRowsPlan& p, const EvictStep* ev, hipStream_t st) {
+  return a.dm.D == 128 ? launch_form<128>(a, p, ev, st) : launch_form<64>(a, p, ev, st);
 }
-
-hipError_t launch_few_rows_bf16(const FewRows& a, hipStream_t st) { return a.dm.D == 128 ? launch_all<128>(a, st) : launch_all<64>(a, st); }
 
 }  // namespace citrus

@@ -1,83 +1,73 @@
-// Generation over a retained cache: attention of drafted trees and of single tokens, the commit of an accepted path.
+// Generation over a retained cache: how the attention of drafted trees and of single tokens is launched, the joining of key ranges, the
+// commit of an accepted path.
 //
 //   S[t, j] = scale q_t . k_j,   out_t = sum_j softmax_j(S[t, .]) v_j
 // over the states j of the row's document: its first len cache rows, then the draft rows that the node's word names.
-#include "bf16_math.h"
 #include "few_rows.h"
 
 namespace citrus {
 namespace {
 
-__device__ inline void store_piece(uint16_t* p, const Piece<uint16_t>& f) {
-  uint4 w;
-  w.x = pack_bf16x2(f.x[0], f.x[1]);
-  w.y = pack_bf16x2(f.x[2], f.x[3]);
-  w.z = pack_bf16x2(f.x[4], f.x[5]);
-  w.w = pack_bf16x2(f.x[6], f.x[7]);
-  *reinterpret_cast<uint4*>(p) = w;
-}
-__device__ inline void store_piece(float* p, const Piece<float>& f) {
-  *reinterpret_cast<float4*>(p) = make_float4(f.x[0], f.x[1], f.x[2], f.x[3]);
+// One thread per four elements of a row.  grid: (.., B * L)
+template <typename E, int D>
+__global__ __launch_bounds__(256) void join_ranges_kernel(FewRows a) {
+  const Dims& dm = a.dm;
+  const int nodes = a.ks.c, e = blockIdx.x * 256 + threadIdx.x;
+  if (e >= dm.Hq * nodes * (D / 4)) return;
+  const int d = e % (D / 4) * 4, r = e / (D / 4);
+  const int64_t row = static_cast<int64_t>(blockIdx.y) * dm.Hq * nodes + r;
+  RowParts p = join_ranges<D>(a, row, d);
+  finish_row<E>(a, blockIdx.y / dm.L, blockIdx.y % dm.L, r / nodes, r % nodes, row, d, p);
 }
 
-// One wave per query row: the lanes that share a state hold a 16-byte piece of its row each, the groups of lanes take the
-// states in turn and keep a running (maximum, sum, output) of their own, merged at the end.
-template <typename E, int D>
-__global__ __launch_bounds__(256) void few_rows_kernel(FewRows a) {
-  typedef Piece<E> P;
-  constexpr int kPieces = D / P::kN, kGroups = 64 / kPieces;
-  const Dims& dm = a.dm;
-  const int lane = threadIdx.x % 64, piece = lane % kPieces, group = lane / kPieces;
-  const int rows = dm.Hq * a.ks.c;
-  const int row = blockIdx.x * 4 + threadIdx.x / 64;
-  if (row >= rows) return;
-  const int b = blockIdx.y / dm.L, l = blockIdx.y % dm.L, h = row / a.ks.c, t = row % a.ks.c, g = h / dm.G;
-  const int n_c = a.lens != nullptr ? min(max(a.lens[b], 0), a.ks.n_c) : a.ks.n_c;
-  const uint64_t word = a.words != nullptr ? a.words[b * a.words_sb + t] : 1;
-  const bool real = word >> t & 1;
-  const int n = real ? n_c + a.ks.c : 0;
-  const P q = load_piece(row_ptr<E>(a.q, b, l, h, t) + piece * P::kN);
-  float m = -INFINITY, sum = 0.f;
-  P acc = {};
-  for (int j = group; j < n; j += kGroups) {
-    if (j >= n_c && !(word >> (j - n_c) & 1)) continue;
-    const bool cached = j < n_c;
-    const int64_t r = cached ? j : j - n_c;
-    const P k = load_piece(row_ptr<E>(cached ? a.ks.cache : a.ks.chunk, b, l, g, r) + piece * P::kN);
-    const P v = load_piece(row_ptr<E>(cached ? a.vs.cache : a.vs.chunk, b, l, g, r) + piece * P::kN);
-    float s = 0.f;
-#pragma unroll
-    for (int x = 0; x < P::kN; ++x) s = fmaf(q.x[x], k.x[x], s);
-#pragma unroll
-    for (int o = kPieces / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-    s *= dm.scale * kLog2e;
-    if (a.scores != nullptr && piece == 0) a.scores[(static_cast<int64_t>(blockIdx.y) * dm.Hq + h) * a.score_pitch + j] = s;
-    const float m_new = fmaxf(m, s), safe = m_new == -INFINITY ? 0.f : m_new;
-    const float old = exp2f(m - safe), p = exp2f(s - safe);
-    sum = fmaf(sum, old, p);
-#pragma unroll
-    for (int x = 0; x < P::kN; ++x) acc.x[x] = fmaf(acc.x[x], old, p * v.x[x]);
-    m = m_new;
+constexpr int kMostSplits = 64;
+// Workgroups that the chip holds: one to a compute unit for bf16 at head_dim 128 (LDS), else two.
+int64_t slots_of(int dtype, const Dims& dm) { return dtype == CITRUS_BF16 && dm.D == 128 ? 256 : 512; }
+
+FewRowsPlan form_of(int dtype, const Dims& dm, int nodes, bool logits) {
+  const int blocks = (dm.G * nodes + 31) / 32;
+  FewRowsPlan p{};
+  const bool alone = blocks == 1 || logits || dtype == CITRUS_F32;  // a block of 32 rows to a workgroup
+  p.waves = alone || blocks == 2 ? 4 : 8;
+  p.kh = alone ? 4 : blocks <= 4 ? 2 : 1;
+  const int per = p.waves / p.kh;
+  p.row_groups = (blocks + per - 1) / per;
+  return p;
+}
+int64_t workgroups(const Dims& dm, const FewRowsPlan& p) { return static_cast<int64_t>(dm.B) * dm.L * dm.Hkv * p.row_groups; }
+int most_splits(int dtype, const Dims& dm, const FewRowsPlan& p) {
+  const int64_t s = 4 * slots_of(dtype, dm) / workgroups(dm, p);
+  return static_cast<int>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
+}
+
+// Ranges of keys.  Rounds of the chip times a workgroup's share of the keys is what a launch takes; another launch to join the ranges
+// costs about as much as eight 32-key tiles of a workgroup's stream, an eviction's own launch fourteen, an eviction within the launch four.
+FewRowsPlan plan_for(int dtype, const Dims& dm, int nodes, int most_keys, bool logits, bool may_evict) {
+  FewRowsPlan p = form_of(dtype, dm, nodes, logits);
+  const int64_t groups = workgroups(dm, p), slots = slots_of(dtype, dm);
+  const int unit = p.kh == 4 ? 32 : 64, tiles = (most_keys + unit - 1) / unit;
+  int64_t best = INT64_MAX;
+  for (int s = 1; s <= most_splits(dtype, dm, p); ++s) {
+    const int per = (tiles + s - 1) / s;
+    if (s > 1 && per * unit < 128) break;
+    if ((tiles + per - 1) / per != s) continue;  // no empty ranges
+    const int behind = logits ? (s == 1 && may_evict ? 4 : 14) : s > 1 ? 8 : 0;
+    const int64_t cost = (s * groups + slots - 1) / slots * (per * unit / 32 + 6 + (s == 1 && may_evict ? 4 : 0)) + (behind == 4 ? 0 : behind);
+    if (cost < best) best = cost, p.splits = s;
   }
-#pragma unroll
-  for (int o = kPieces; o < 64; o <<= 1) {
-    const float m2 = __shfl_xor(m, o, 64), sum2 = __shfl_xor(sum, o, 64);
-    const float top = fmaxf(m, m2), safe = top == -INFINITY ? 0.f : top;
-    const float e1 = exp2f(m - safe), e2 = exp2f(m2 - safe);
-    sum = sum * e1 + sum2 * e2;
-#pragma unroll
-    for (int x = 0; x < P::kN; ++x) acc.x[x] = acc.x[x] * e1 + __shfl_xor(acc.x[x], o, 64) * e2;
-    m = top;
+  p.evicts = may_evict && p.splits == 1;
+  return p;
+}
+
+hipError_t launch_main(int dtype, FewRows& a, const FewRowsPlan& p, const EvictStep* ev, hipStream_t st) {
+  a.splits = p.splits;
+  a.part_o = nullptr;
+  if (p.splits > 1 || (ev != nullptr && !p.evicts)) {
+    const size_t rows = static_cast<size_t>(p.splits) * a.dm.B * a.dm.L * a.dm.Hq * a.ks.c;
+    a.part_o = a.workspace;
+    a.part_ml = reinterpret_cast<float2*>(a.workspace + rows * a.dm.D);
   }
-#pragma unroll
-  for (int x = 0; x < P::kN; ++x) acc.x[x] = real ? acc.x[x] / sum : 0.f;
-  if (group == 0) store_piece(const_cast<E*>(row_ptr<E>(a.out, b, l, h, t)) + piece * P::kN, acc);
-  if (lane == 0) {
-    const int64_t at = (static_cast<int64_t>(blockIdx.y) * dm.Hq + h) * a.ks.c + t;
-    const float lse2 = real ? m + log2f(sum) : -INFINITY;
-    if (a.lse != nullptr) a.lse[at] = lse2 * kLn2;
-    if (a.lse2 != nullptr) a.lse2[at] = lse2;
-  }
+  return dtype == CITRUS_BF16 ? launch_few_rows_bf16(a, p, ev, st) : launch_few_rows_f32(a, p, ev, st);
 }
 
 // The accepted path's rows: row len + i of a document's cache takes draft row path[i], i < accepted.
@@ -106,15 +96,32 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(Dims dm, View kd, View
 }  // namespace
 
 size_t few_rows_workspace_floats(int dtype, const Dims& dm, int rows) {
-  return dtype == CITRUS_BF16 ? few_rows_bf16_workspace_floats(dm, rows) : 0;
+  size_t most = 0;
+  for (int t = 1; t <= rows; ++t)
+    for (const bool logits : {false, true}) {
+      if (logits && t > 1) continue;
+      const int s = most_splits(dtype, dm, form_of(dtype, dm, t, logits));
+      const size_t f = s == 1 && !logits ? 0 : static_cast<size_t>(s) * dm.B * dm.L * dm.Hq * t * (dm.D + 2);
+      if (f > most) most = f;
+    }
+  return most;
 }
 
-hipError_t launch_few_rows(int dtype, const FewRows& a, hipStream_t st) {
-  if (dtype == CITRUS_BF16) return launch_few_rows_bf16(a, st);
-  const dim3 grid((a.dm.Hq * a.ks.c + 3) / 4, a.dm.B * a.dm.L);
-  const auto kernel = a.dm.D == 128 ? few_rows_kernel<float, 128> : few_rows_kernel<float, 64>;
-  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
+hipError_t launch_tree_attn(int dtype, FewRows a, hipStream_t st) {
+  const FewRowsPlan p = plan_for(dtype, a.dm, a.ks.c, a.ks.n_c + a.ks.c, false, false);
+  const hipError_t e = launch_main(dtype, a, p, nullptr, st);
+  if (e != hipSuccess || p.splits == 1) return e;
+  const auto join = dtype == CITRUS_BF16 ? (a.dm.D == 128 ? join_ranges_kernel<uint16_t, 128> : join_ranges_kernel<uint16_t, 64>)
+                                         : (a.dm.D == 128 ? join_ranges_kernel<float, 128> : join_ranges_kernel<float, 64>);
+  const int pieces = a.dm.Hq * a.ks.c * (a.dm.D / 4);
+  hipLaunchKernelGGL(join, dim3((pieces + 255) / 256, a.dm.B * a.dm.L), dim3(256), 0, st, a);
   return hipGetLastError();
+}
+
+hipError_t launch_decode_evict(int dtype, FewRows a, const EvictStep& ev, bool per_layer, hipStream_t st) {
+  const FewRowsPlan p = plan_for(dtype, a.dm, 1, a.ks.n_c + 1, true, !per_layer && a.dm.G <= 32);
+  const hipError_t e = launch_main(dtype, a, p, &ev, st);
+  return e != hipSuccess || p.evicts ? e : launch_evict_step(dtype, a, ev, per_layer, st);
 }
 
 hipError_t launch_tree_commit(int elem_bytes, const Dims& dm, View k_draft, View v_draft, View k_cache, View v_cache,
