@@ -200,8 +200,6 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
   // this lane's row: node t of head h
   const int row = (row_group * kBlocks + wu / KH) * 32 + col;
   const int h = g * dm.G + min(row, rows - 1) / nodes, t = min(row, rows - 1) % nodes;
-  uint64_t word = a.words != nullptr ? a.words[b * a.words_sb + t] : 1;
-  if (nodes < 64) word &= (uint64_t{1} << nodes) - 1;
   const bool idle = (row_group * kBlocks + wu / KH) * 32 >= rows;  // a wave without rows helps to load
 
   const int k_ss_cache = static_cast<int>(a.ks.cache.ss), k_ss_own = static_cast<int>(a.ks.chunk.ss);
@@ -241,27 +239,6 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
   };
   const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char_ptr)lds));
 
-  // per-lane LDS read offsets inside a tile, swizzle included
-  uint32_t k_off[T::kKk], v_off[2 * T::kOut];
-#pragma unroll
-  for (int kk = 0; kk < T::kKk; ++kk) k_off[kk] = col * T::kRowBytes + (((2 * kk + grp) ^ T::swz(col)) * 16);
-  const int s16 = lane % 16, q16 = lane / 16;
-  const int v_cl = (T::kSegs / 2 * (q16 % 2) + (s16 % 4) / 2) ^ T::swz(4 * (q16 / 2) + s16 / 4);
-#pragma unroll
-  for (int e = 0; e < 2 * T::kOut; ++e) v_off[e] = (4 * (q16 / 2) + s16 / 4) * T::kRowBytes + ((e ^ v_cl) * 16) + 8 * (s16 % 2);
-
-  bf16x8 q_op[T::kKk];
-  {
-    const uint16_t* qp = row_ptr<uint16_t>(a.q, b, l, h, t) + 8 * grp;
-#pragma unroll
-    for (int kk = 0; kk < T::kKk; ++kk) {
-      Pack8 x;
-      x.u = *reinterpret_cast<const uint4*>(qp + 16 * kk);
-      q_op[kk] = x.v;
-    }
-  }
-  wait_loads<0>();  // the operand has landed before the first tile is asked for
-
   const float c2 = dm.scale * kLog2e;
   Column<D> c;
   float* scores = nullptr;  // of this lane's row
@@ -272,6 +249,32 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
   }
 
   auto over_the_keys = [&]<bool CAREFUL>() {
+    int at_lane = lane;
+    asm volatile("" : "+v"(at_lane));  // what follows from it is formed anew by the second pass: kept for it, it cost the first registers
+    const int at_col = at_lane % 32, at_grp = at_lane / 32;
+    const int at_row = min((row_group * kBlocks + wu / KH) * 32 + at_col, rows - 1), at_t = at_row % nodes;
+    uint64_t word = a.words != nullptr ? a.words[b * a.words_sb + at_t] : 1;
+    if (nodes < 64) word &= (uint64_t{1} << nodes) - 1;
+    // per-lane LDS read offsets inside a tile, swizzle included
+    uint32_t k_off[T::kKk], v_off[2 * T::kOut];
+#pragma unroll
+    for (int kk = 0; kk < T::kKk; ++kk) k_off[kk] = at_col * T::kRowBytes + (((2 * kk + at_grp) ^ T::swz(at_col)) * 16);
+    const int s16 = at_lane % 16, q16 = at_lane / 16;
+    const int v_cl = (T::kSegs / 2 * (q16 % 2) + (s16 % 4) / 2) ^ T::swz(4 * (q16 / 2) + s16 / 4);
+#pragma unroll
+    for (int e = 0; e < 2 * T::kOut; ++e) v_off[e] = (4 * (q16 / 2) + s16 / 4) * T::kRowBytes + ((e ^ v_cl) * 16) + 8 * (s16 % 2);
+
+    bf16x8 q_op[T::kKk];
+    auto load_queries = [&] {  // while the first keys are on their way; what is asked for later is counted from here
+      const uint16_t* qp = row_ptr<uint16_t>(a.q, b, l, g * dm.G + at_row / nodes, at_t) + 8 * at_grp;
+#pragma unroll
+      for (int kk = 0; kk < T::kKk; ++kk) {
+        Pack8 x;
+        x.u = *reinterpret_cast<const uint4*>(qp + 16 * kk);
+        q_op[kk] = x.v;
+      }
+      wait_loads<0>();
+    };
     c.m = -INFINITY;
     c.l = 0.f;
 #pragma unroll
@@ -299,6 +302,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
       };
       int x = sp * per + wu;
       if (x < end) fill_tile(x, 0);
+      load_queries();
       for (int it = 0; x < end; x += WAVES, ++it) {
         const int buf = it & 1;
         // the other buffer was last read in the previous turn, whose reads have all returned
@@ -321,7 +325,9 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
         char* k_t = lds + (x - begin) % kStages * kStageBytes;
         fill(x * kStageKeys, wu * kGroups, kGroups, k_t, k_t + kSub * kTileBytes);
       };
-      for (int x = begin; x < min(end, begin + kStages - 1); ++x) fill_stage(x);
+      if (begin < end) fill_stage(begin);
+      load_queries();
+      for (int x = begin + 1; x < min(end, begin + kStages - 1); ++x) fill_stage(x);
       for (int x = begin; x < end; ++x) {
         // this wave's loads of the stage have landed; behind the barrier everybody's have, and the stage before has been read
         if (x + kStages - 2 < end)
@@ -347,7 +353,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
   for (int r = 0; r < T::kOut; ++r)
 #pragma unroll
     for (int i = 0; i < 16; ++i) finite &= fabsf(c.o[r][i]) < INFINITY;
-  if (!__syncthreads_and(finite || row >= rows || !(word >> t & 1))) over_the_keys.template operator()<true>();
+  const bool real = a.words == nullptr || (a.words[b * a.words_sb + t] >> t & 1);
+  if (!__syncthreads_and(finite || row >= rows || !real)) over_the_keys.template operator()<true>();
 
   // ---- the waves of a block of rows join through LDS (the tiles have been read when every wave is here) ----
   constexpr int kPitch = D + 4;
