@@ -8,6 +8,7 @@
 #include <atomic>
 
 #include "citrus.h"
+#include "fast_div.h"
 
 namespace citrus {
 
@@ -155,6 +156,7 @@ struct FewRows {
   float* workspace;       // few_rows_workspace_floats
   // of the launch: ranges of keys, and where their parts of the rows go (NULL: there is one, and it finishes its rows)
   int splits;
+  FastDiv by_splits, by_layers, by_nodes;
   float2* part_ml;        // [range][B*L*Hq*c]: maximum (base 2), sum
   float* part_o;          // [range][B*L*Hq*c][D]
 };

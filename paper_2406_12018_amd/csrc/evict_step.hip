@@ -14,7 +14,7 @@ __device__ inline void rows_of_unit(const FewRows& a, int b, int l, int g, bool 
     for (int x = threadIdx.x; x < G * (D / 4); x += THREADS) {
       const int h = x / (D / 4), d = x % (D / 4) * 4;
       RowParts p = join_ranges<D>(a, row0 + h, d);
-      finish_row<E>(a, b, l, g * G + h, 0, row0 + h, d, p, lse2 + h);
+      finish_row<E>(a, b, l, g * G + h, 0, row0 + h, d, p, true, lse2 + h);
     }
   } else {
     const int64_t all = static_cast<int64_t>(a.dm.B) * a.dm.L * a.dm.Hq;
@@ -33,11 +33,13 @@ constexpr int kUnitThreads = 512;
 template <typename E, int D>
 __global__ __launch_bounds__(kUnitThreads) void evict_unit_kernel(FewRows a, EvictStep e) {
   extern __shared__ float lse2[];
-  __shared__ Candidate scratch[kUnitThreads / 64 + 1];
-  const int g = blockIdx.x, b = blockIdx.y / a.dm.L, l = blockIdx.y % a.dm.L;
+  __shared__ EvictLds<kUnitThreads> lds;
+  const int g = blockIdx.x, b = a.by_layers.quotient(blockIdx.y), l = blockIdx.y - b * a.dm.L;
+  EvictAhead<kUnitThreads> ahead;
+  ahead.ask(e, b, l, g);
   rows_of_unit<E, D, kUnitThreads>(a, b, l, g, true, lse2);
   const float* scores = a.scores + (static_cast<int64_t>(blockIdx.y) * a.dm.Hq + g * a.dm.G) * a.score_pitch;
-  evict_unit<kUnitThreads>(e, b, l, g, scores, a.score_pitch, lse2, scratch);
+  evict_unit<kUnitThreads>(e, b, l, g, scores, a.score_pitch, lse2, ahead, lds);
 }
 
 // Long caches and selections per layer: the sums grow in ranges of keys, and one workgroup per selection makes room behind them.
@@ -47,21 +49,25 @@ constexpr int kRangeKeys = 4096;
 template <typename E, int D>
 __global__ __launch_bounds__(kThreads) void grow_sums_kernel(FewRows a, EvictStep e, int ranges) {
   extern __shared__ float lse2[];
-  __shared__ Candidate scratch[kThreads / 64];
-  const int g = blockIdx.x / ranges, range = blockIdx.x % ranges, b = blockIdx.y / a.dm.L, l = blockIdx.y % a.dm.L;
+  __shared__ EvictLds<kThreads> lds;
+  const int g = blockIdx.x / ranges, range = blockIdx.x % ranges, b = a.by_layers.quotient(blockIdx.y), l = blockIdx.y - b * a.dm.L;
   const int64_t unit = static_cast<int64_t>(blockIdx.y) * a.dm.Hkv + g;
+  float* const acc = e.acc + unit * e.acc_pitch;
+  const int begin = range * kRangeKeys, end = min(e.n + 1, begin + kRangeKeys);
+  const Sums4 sums = load_sums(e, acc, begin + 4 * threadIdx.x);
   rows_of_unit<E, D, kThreads>(a, b, l, g, range == 0, lse2);
   const float* scores = a.scores + unit * a.dm.G * a.score_pitch;
-  const int begin = range * kRangeKeys, end = min(e.n + 1, begin + kRangeKeys);
-  Candidate best = grow_sums<kThreads>(e, scores, a.score_pitch, lse2, e.acc + unit * e.acc_pitch, begin, end, e.own + unit);
-  if (e.oldest < 0) return;
-  best = smallest_of_block<kThreads>(best, scratch);
-  if (threadIdx.x == 0) e.best[unit * ranges + range] = make_float2(best.sum, __int_as_float(best.slot));
+  const Candidate mine = grow_sums<kThreads>(e, scores, a.score_pitch, lse2, acc, begin, end, sums, lds);
+  const Candidate best = smallest_of_block<kThreads>(mine, lds);
+  if (threadIdx.x == 0) {
+    e.best[unit * ranges + range] = make_float2(best.sum, __int_as_float(best.slot));
+    if (end == e.n + 1) e.own[unit] = lds.own;
+  }
 }
 // grid: (Hkv / heads, B * L): the smallest of the ranges' candidates, or of a layer's sums over its heads
 __global__ __launch_bounds__(kThreads) void make_room_kernel(EvictStep e, int ranges, int heads) {
-  __shared__ Candidate scratch[kThreads / 64];
-  const int g0 = blockIdx.x * heads;
+  __shared__ EvictLds<kThreads> lds;
+  const int g0 = blockIdx.x * heads, b = blockIdx.y / e.dm.L, l = blockIdx.y % e.dm.L;
   const int64_t unit0 = static_cast<int64_t>(blockIdx.y) * e.dm.Hkv + g0;
   int slot = -1;
   if (e.oldest >= 0) {
@@ -73,16 +79,19 @@ __global__ __launch_bounds__(kThreads) void make_room_kernel(EvictStep e, int ra
       }
     } else {
       for (int j = threadIdx.x; j < e.n; j += kThreads) {
-        if (!may_go(e, j)) continue;
         float sum = 0.f;
 #pragma unroll 8
         for (int h = 0; h < heads; ++h) sum += e.acc[(unit0 + h) * e.acc_pitch + j];
-        best = smaller(best, Candidate{sum, j});
+        if (may_go(e, j)) best = smaller(best, Candidate{sum, j});
       }
     }
-    slot = smallest_of_block<kThreads>(best, scratch).slot;
+    slot = smallest_of_block<kThreads>(best, lds).slot;
   }
-  move_states<kThreads>(e, blockIdx.y / e.dm.L, blockIdx.y % e.dm.L, g0, heads, slot, e.own + unit0);
+  for (int x = threadIdx.x; x < heads * 2 * e.row_bytes / 16; x += kThreads) move_piece(e, moving_piece(e, b, l, g0, x), slot);
+  for (int h = threadIdx.x; h < heads; h += kThreads) {
+    float* const acc = e.acc + (unit0 + h) * e.acc_pitch;
+    move_sum(e, acc, slot, slot >= 0 ? acc[e.oldest] : 0.f, e.own[unit0 + h]);
+  }
   if (threadIdx.x == 0 && e.evicted != nullptr) e.evicted[static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x] = slot;
 }
 

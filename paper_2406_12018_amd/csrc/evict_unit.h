@@ -2,10 +2,12 @@
 // them.
 //
 //   w_j = sum over the heads of the group of exp2(s_j - lse),   sum_j += w_j
-// and the state with the smallest sum makes room for the token's.
+// and the state with the smallest sum makes room for the token's.  Everything that is read is asked for before it is needed: what this
+// costs behind a stream of keys is the exchange between the waves.
 #pragma once
 
 #include "few_rows.h"
+#include "lanes.h"
 
 namespace citrus {
 namespace {
@@ -18,33 +20,64 @@ struct Candidate {
 __device__ inline Candidate smaller(const Candidate& a, const Candidate& b) {
   return b.sum < a.sum || (b.sum == a.sum && b.slot < a.slot) ? b : a;
 }
+template <int F>
+__device__ inline Candidate smaller_by_lane(const Candidate& c) {
+  return smaller(c, Candidate{from_lane<F>(c.sum), __float_as_int(from_lane<F>(__int_as_float(c.slot)))});
+}
+__device__ inline Candidate smallest_of_wave(Candidate c) {
+  c = smaller_by_lane<kXor1>(c);
+  c = smaller_by_lane<kXor2>(c);
+  c = smaller_by_lane<kXor7>(c);  // l ^ 4 holds what l ^ 7 does
+  c = smaller_by_lane<kXor8>(c);
+  float s0, s1, j0, j1;
+  both_of_rows(c.sum, s0, s1);
+  both_of_rows(__int_as_float(c.slot), j0, j1);
+  c = smaller(Candidate{s0, __float_as_int(j0)}, Candidate{s1, __float_as_int(j1)});
+  both_of_halves(c.sum, s0, s1);
+  both_of_halves(__int_as_float(c.slot), j0, j1);
+  return smaller(Candidate{s0, __float_as_int(j0)}, Candidate{s1, __float_as_int(j1)});
+}
 __device__ inline bool may_go(const EvictStep& e, int slot) {
   return (slot >= e.start && slot < e.n - e.recent) || slot == e.oldest;
 }
-// scratch: a Candidate per wave; the workgroup is in step on return
+
+// LDS of a workgroup that evicts.
 template <int THREADS>
-__device__ inline Candidate smallest_of_block(Candidate c, Candidate* scratch) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) c = smaller(c, Candidate{__shfl_xor(c.sum, o, 64), __shfl_xor(c.slot, o, 64)});
-  if (threadIdx.x % 64 == 0) scratch[threadIdx.x / 64] = c;
+struct EvictLds {
+  Candidate best[THREADS / 64];
+  float own, oldest;  // the token's weight, the sum of the oldest recent state
+};
+// the workgroup is in step on return
+template <int THREADS>
+__device__ inline Candidate smallest_of_block(Candidate c, EvictLds<THREADS>& lds) {
+  c = smallest_of_wave(c);
+  if (threadIdx.x % 64 == 0) lds.best[threadIdx.x / 64] = c;
   __syncthreads();
-  c = scratch[0];
+  c = lds.best[0];
 #pragma unroll
-  for (int w = 1; w < THREADS / 64; ++w) c = smaller(c, scratch[w]);
+  for (int w = 1; w < THREADS / 64; ++w) c = smaller(c, lds.best[w]);
   return c;
 }
 
-// Sums of the keys [begin, end) of a unit grow, four keys a thread and turn; begin is a multiple of 4.  scores: [head][score_pitch],
-// lse2: by head.  Returns this thread's smallest; own: the token's weight, to the thread whose key it is.
+struct Sums4 {
+  float x[4];
+};
+__device__ inline Sums4 load_sums(const EvictStep& e, const float* acc, int j) {
+  Sums4 s;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) s.x[x] = acc[max(min(j + x, e.n - 1), 0)];
+  return s;
+}
+// Sums of the keys [begin, end) of a unit grow, four keys a thread and turn; begin is a multiple of 4.  scores: [head][pitch], lse2: by
+// head.  old: load_sums of the thread's first keys.  Returns this thread's smallest.
 template <int THREADS>
 __device__ inline Candidate grow_sums(const EvictStep& e, const float* scores, int64_t pitch, const float* lse2, float* acc, int begin, int end,
-                                      float* own) {
+                                      Sums4 old, EvictLds<THREADS>& lds) {
   const int G = e.dm.G;
   Candidate best{INFINITY, e.oldest};
   for (int j = begin + 4 * threadIdx.x; j < end; j += 4 * THREADS) {
-    float old[4], w[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int x = 0; x < 4; ++x) old[x] = acc[min(j + x, e.n - 1 > 0 ? e.n - 1 : 0)];
+    const Sums4 next = load_sums(e, acc, j + 4 * THREADS);
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int h = 0; h < G; ++h) {
       const float4 s = *reinterpret_cast<const float4*>(scores + h * pitch + j);
@@ -57,54 +90,73 @@ __device__ inline Candidate grow_sums(const EvictStep& e, const float* scores, i
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       if (j + x < e.n) {
-        const float sum = old[x] + w[x];
+        const float sum = old.x[x] + w[x];
         acc[j + x] = sum;
         if (may_go(e, j + x)) best = smaller(best, Candidate{sum, j + x});
+        if (j + x == e.oldest) lds.oldest = sum;
       } else if (j + x == e.n) {
-        *own = w[x];
+        lds.own = w[x];
       }
     }
+    old = next;
   }
   return best;
 }
 
-// Slot `slot` (-1: none) of `heads` heads from g0 on takes the oldest recent state, that one's place (or the row behind the cache) the
-// token's.  own: the token's weights by head.
-template <int THREADS>
-__device__ inline void move_states(const EvictStep& e, int b, int l, int g0, int heads, int slot, const float* own) {
-  const int to = e.oldest >= 0 ? e.oldest : e.n;
-  const int esz = e.row_bytes / e.dm.D, pieces = e.row_bytes / 16;
-  for (int x = threadIdx.x; x < heads * 2 * pieces; x += THREADS) {
-    const int g = g0 + x / (2 * pieces), piece = x % pieces;
-    const bool is_v = x / pieces % 2;
-    const View &from = is_v ? e.v_new : e.k_new, &cache = is_v ? e.v_cache : e.k_cache;
-    char* rows = static_cast<char*>(const_cast<void*>(cache.ptr)) + (b * cache.sb + l * cache.sl + g * cache.sh) * esz;
-    const char* src = static_cast<const char*>(from.ptr) + (b * from.sb + l * from.sl + g * from.sh) * esz;
-    uint4* at = reinterpret_cast<uint4*>(rows + to * cache.ss * esz) + piece;
-    const uint4 fresh = reinterpret_cast<const uint4*>(src)[piece], moved = slot >= 0 ? *at : fresh;
-    if (slot >= 0 && slot != to) *(reinterpret_cast<uint4*>(rows + slot * cache.ss * esz) + piece) = moved;
-    *at = fresh;
-  }
-  const int64_t unit0 = static_cast<int64_t>(b * e.dm.L + l) * e.dm.Hkv + g0;
-  for (int h = threadIdx.x; h < heads; h += THREADS) {
-    float* acc = e.acc + (unit0 + h) * e.acc_pitch;
-    if (slot >= 0) acc[slot] = acc[to];
-    acc[to] = own[h];
-  }
+// A 16-byte piece of what moves: of the oldest recent state, and of the token's.
+struct MovingPiece {
+  uint4 *from, fresh, moved;
+  char* rows;  // the piece of row 0
+  int64_t pitch;
+};
+// x: head * 2 * pieces of a row + (K or V) * pieces + piece
+__device__ inline MovingPiece moving_piece(const EvictStep& e, int b, int l, int g0, int x) {
+  const int esz = e.row_bytes / e.dm.D, pieces = e.row_bytes / 16;  // powers of two
+  const int bits = __builtin_ctz(pieces), g = g0 + (x >> (bits + 1)), piece = x & (pieces - 1);
+  const bool is_v = x >> bits & 1;
+  const View &from = is_v ? e.v_new : e.k_new, &cache = is_v ? e.v_cache : e.k_cache;
+  MovingPiece p;
+  p.rows = static_cast<char*>(const_cast<void*>(cache.ptr)) + (b * cache.sb + l * cache.sl + g * cache.sh) * esz + 16 * piece;
+  p.pitch = cache.ss * esz;
+  const char* src = static_cast<const char*>(from.ptr) + (b * from.sb + l * from.sl + g * from.sh) * esz + 16 * piece;
+  p.from = reinterpret_cast<uint4*>(p.rows + (e.oldest >= 0 ? e.oldest : e.n) * p.pitch);
+  p.fresh = *reinterpret_cast<const uint4*>(src);
+  p.moved = e.oldest >= 0 ? *p.from : p.fresh;
+  return p;
+}
+__device__ inline void move_piece(const EvictStep& e, const MovingPiece& p, int slot) {
+  if (slot >= 0 && slot != e.oldest) *reinterpret_cast<uint4*>(p.rows + slot * p.pitch) = p.moved;
+  *p.from = p.fresh;
+}
+// ... and of the sums
+__device__ inline void move_sum(const EvictStep& e, float* acc, int slot, float oldest, float own) {
+  if (slot >= 0) acc[slot] = oldest;
+  acc[e.oldest >= 0 ? e.oldest : e.n] = own;
 }
 
-// The whole unit.  lse2: by head, in LDS; scratch (LDS): Candidates of the waves and the token's weight behind them.  acc is read by
-// threads other than the ones that wrote it, behind a barrier.
+// The whole unit, by THREADS threads (at least the pieces of a K and a V row).  Asked for ahead: its first sums and what moves.
+template <int THREADS>
+struct EvictAhead {
+  Sums4 sums;
+  MovingPiece piece;
+  __device__ void ask(const EvictStep& e, int b, int l, int g) {
+    sums = load_sums(e, e.acc + (static_cast<int64_t>(b * e.dm.L + l) * e.dm.Hkv + g) * e.acc_pitch, 4 * threadIdx.x);
+    if (threadIdx.x < 2 * e.row_bytes / 16) piece = moving_piece(e, b, l, g, threadIdx.x);
+  }
+};
 template <int THREADS>
 __device__ inline void evict_unit(const EvictStep& e, int b, int l, int g, const float* scores, int64_t pitch, const float* lse2,
-                                  Candidate* scratch) {
+                                  const EvictAhead<THREADS>& ahead, EvictLds<THREADS>& lds) {
   const int64_t unit = static_cast<int64_t>(b * e.dm.L + l) * e.dm.Hkv + g;
-  float* const own = reinterpret_cast<float*>(scratch + THREADS / 64);
-  Candidate best = grow_sums<THREADS>(e, scores, pitch, lse2, e.acc + unit * e.acc_pitch, 0, e.n + 1, own);
-  best = smallest_of_block<THREADS>(best, scratch);
+  float* const acc = e.acc + unit * e.acc_pitch;
+  Candidate best = grow_sums<THREADS>(e, scores, pitch, lse2, acc, 0, e.n + 1, ahead.sums, lds);
+  best = smallest_of_block<THREADS>(best, lds);
   const int slot = e.oldest >= 0 ? best.slot : -1;
-  move_states<THREADS>(e, b, l, g, 1, slot, own);
-  if (threadIdx.x == 0 && e.evicted != nullptr) e.evicted[unit] = slot;
+  if (threadIdx.x < 2 * e.row_bytes / 16) move_piece(e, ahead.piece, slot);
+  if (threadIdx.x == 0) {
+    move_sum(e, acc, slot, lds.oldest, lds.own);
+    if (e.evicted != nullptr) e.evicted[unit] = slot;
+  }
 }
 
 }  // namespace

@@ -38,40 +38,52 @@ struct RowParts {
   }
 };
 
+// Is there a node t in document b?
+__device__ inline bool is_node(const FewRows& a, int b, int t) { return a.words == nullptr || (a.words[b * a.words_sb + t] >> t & 1); }
+
 // Four elements of a row's result, and with the first of them its log-sum-exp.
 template <typename E>
-__device__ inline void finish_row(const FewRows& a, int b, int l, int h, int t, int64_t row, int d, RowParts& r, float* lse2 = nullptr) {
-  const bool real = a.words == nullptr || (a.words[b * a.words_sb + t] >> t & 1);
+__device__ inline void finish_row(const FewRows& a, int b, int l, int h, int t, int64_t row, int d, RowParts& r, bool real, float* lse2 = nullptr) {
+  const float inv = 1.f / r.sum;
 #pragma unroll
-  for (int x = 0; x < 4; ++x) r.o[x] = real ? r.o[x] / r.sum : 0.f;
+  for (int x = 0; x < 4; ++x) r.o[x] = real ? r.o[x] * inv : 0.f;
   store4(const_cast<E*>(row_ptr<E>(a.out, b, l, h, t)) + d, r.o);
   if (d == 0) {
-    const float v = real ? r.reference() + log2f(r.sum) : -INFINITY;
+    const float v = real ? r.reference() + __builtin_amdgcn_logf(r.sum) : -INFINITY;
     if (a.lse != nullptr) a.lse[row] = v * kLn2;
     if (lse2 != nullptr) *lse2 = v;
   }
 }
 
-// The waves of a workgroup have left their parts in LDS, o_s[wave][32 rows][D + 4] and ml_s[wave][32]; KH of them share a block of 32 rows.
-// The workgroup's `here` rows from `first` on of KV head g; lse2 (optional, LDS): base 2, by row of this workgroup.
+// What the waves of a workgroup leave in LDS for each other: parts of their rows.
+struct WaveRow {
+  float m, sum;
+  int real, spare;
+};
+// o_s[wave][32 rows][D + 4], rows_s[wave][32]; KH waves share a block of 32 rows.  The workgroup's `here` rows from `first` on of KV head
+// g; lse2 (optional, LDS): base 2, by row of this workgroup.
 template <typename E, int D, int WAVES, int KH>
-__device__ __forceinline__ void join_waves(const FewRows& a, const float* o_s, const float2* ml_s, int g, int first, int here, int sp,
-                                           float* lse2 = nullptr) {
-  constexpr int kPitch = D + 4;
+__device__ __forceinline__ void join_waves(const FewRows& a, const float* o_s, const WaveRow* rows_s, int b, int l, int g, int first, int here,
+                                           int sp, float* lse2 = nullptr) {
+  constexpr int kPitch = D + 4, kRowsAtOnce = 64 * WAVES / (D / 4);
   const Dims& dm = a.dm;
-  const int nodes = a.ks.c, b = blockIdx.y / dm.L, l = blockIdx.y % dm.L;
-  for (int e = threadIdx.x; e < here * (D / 4); e += 64 * WAVES) {
-    const int r = e / (D / 4), d = e % (D / 4) * 4;
+  const int nodes = a.ks.c, bl = b * dm.L + l;
+  const int d = threadIdx.x % (D / 4) * 4;
+#pragma unroll 4
+  for (int r = threadIdx.x / (D / 4); r < here; r += kRowsAtOnce) {
     const int at = (r / 32 * KH) * 32 + r % 32;
     RowParts p;
+    WaveRow w[KH];
 #pragma unroll
-    for (int w = 0; w < KH; ++w) p.m = fmaxf(p.m, ml_s[at + 32 * w].x);
+    for (int x = 0; x < KH; ++x) w[x] = rows_s[at + 32 * x];
 #pragma unroll
-    for (int w = 0; w < KH; ++w) p.add(ml_s[at + 32 * w], *reinterpret_cast<const float4*>(o_s + (at + 32 * w) * kPitch + d));
-    const int h = g * dm.G + (first + r) / nodes, t = (first + r) % nodes;
-    const int64_t row = (static_cast<int64_t>(blockIdx.y) * dm.Hq + h) * nodes + t;
+    for (int x = 0; x < KH; ++x) p.m = fmaxf(p.m, w[x].m);
+#pragma unroll
+    for (int x = 0; x < KH; ++x) p.add(make_float2(w[x].m, w[x].sum), *reinterpret_cast<const float4*>(o_s + (at + 32 * x) * kPitch + d));
+    const int hq = a.by_nodes.quotient(first + r), t = first + r - hq * nodes, h = g * dm.G + hq;
+    const int64_t row = (static_cast<int64_t>(bl) * dm.Hq + h) * nodes + t;
     if (a.part_o == nullptr) {
-      finish_row<E>(a, b, l, h, t, row, d, p, lse2 != nullptr ? lse2 + r : nullptr);
+      finish_row<E>(a, b, l, h, t, row, d, p, w[0].real, lse2 != nullptr ? lse2 + r : nullptr);
     } else {
       const int64_t at_part = static_cast<int64_t>(sp) * dm.B * dm.L * dm.Hq * nodes + row;
       *reinterpret_cast<float4*>(a.part_o + at_part * D + d) = make_float4(p.o[0], p.o[1], p.o[2], p.o[3]);
@@ -85,11 +97,24 @@ template <int D>
 __device__ inline RowParts join_ranges(const FewRows& a, int64_t row, int d) {
   const int64_t all = static_cast<int64_t>(a.dm.B) * a.dm.L * a.dm.Hq * a.ks.c;
   RowParts p;
+#pragma unroll 8
   for (int s = 0; s < a.splits; ++s) p.m = fmaxf(p.m, a.part_ml[s * all + row].x);
-#pragma unroll 4
+#pragma unroll 8
   for (int s = 0; s < a.splits; ++s) p.add(a.part_ml[s * all + row], *reinterpret_cast<const float4*>(a.part_o + (s * all + row) * D + d));
   return p;
 }
+
+// Where a workgroup of the attention is.  grid: (row groups * key ranges, Hkv, B * L)
+struct Place {
+  int sp, row_group, g, b, l;
+  __device__ explicit Place(const FewRows& a) {
+    row_group = a.by_splits.quotient(blockIdx.x);
+    sp = blockIdx.x - row_group * a.splits;
+    g = blockIdx.y;
+    b = a.by_layers.quotient(blockIdx.z);
+    l = blockIdx.z - b * a.dm.L;
+  }
+};
 
 // What a lane sees of the 32 keys from own + n_c on: bit j, by its node's word.
 __device__ inline uint32_t seen_keys(uint64_t word, int own) {

@@ -167,11 +167,11 @@ __device__ __forceinline__ void key_tile(uint32_t k_t, uint32_t v_t, const uint3
 // said it all: an infinite or NaN value then leaves NaN in rows that must be finite, or infinite.  Nothing in the loop looks for such
 // values; a workgroup whose results are not all finite goes over its keys once more, carefully.
 //
-// grid: (row groups * Hkv * key ranges, B * L)
+// grid: (row groups * key ranges, Hkv, B * L)
 template <int D, int WAVES, int KH>
 struct Lds {
-  static constexpr int kRows = WAVES * 32 * (D + 4) * 4, kJoin = kRows + WAVES * 32 * 8;  // o_s, ml_s
-  static constexpr int kAfter = kJoin + 32 * 4 + (WAVES + 1) * 8;                         // lse2, Candidates
+  static constexpr int kRows = WAVES * 32 * (D + 4) * 4, kJoin = kRows + WAVES * 32 * 16;  // o_s, rows_s
+  static constexpr int kAfter = kJoin + 32 * 4 + sizeof(EvictLds<64 * WAVES>);            // lse2
   static constexpr int kTiles = KH == WAVES ? WAVES * Geo<D>::kWaveLdsBytes : kStages * (kStageKeys / 32) * 2 * Geo<D>::kTileBytes;
   static constexpr int kBytes = ((kAfter > kTiles ? kAfter : kTiles) + 15) / 16 * 16;  // ... the strip of logits
 };
@@ -190,16 +190,14 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
   const Dims& dm = a.dm;
   const int lane = threadIdx.x % 64, col = lane % 32, grp = lane / 32;
   const int wu = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int key_splits = a.splits;
-  const int sp = blockIdx.x % key_splits, g = blockIdx.x / key_splits % dm.Hkv, row_group = blockIdx.x / key_splits / dm.Hkv;
-  const int b = blockIdx.y / dm.L, l = blockIdx.y % dm.L;
+  const Place at(a);
+  const int b = at.b, l = at.l, g = at.g, row_group = at.row_group;
   const int nodes = a.ks.c, rows = dm.G * nodes;
   const int n_c = a.lens != nullptr ? min(max(a.lens[b], 0), a.ks.n_c) : a.ks.n_c;
   const int n = n_c + nodes;
 
   // this lane's row: node t of head h
   const int row = (row_group * kBlocks + wu / KH) * 32 + col;
-  const int h = g * dm.G + min(row, rows - 1) / nodes, t = min(row, rows - 1) % nodes;
   const bool idle = (row_group * kBlocks + wu / KH) * 32 >= rows;  // a wave without rows helps to load
 
   const int k_ss_cache = static_cast<int>(a.ks.cache.ss), k_ss_own = static_cast<int>(a.ks.chunk.ss);
@@ -245,15 +243,20 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
   if constexpr (LOGITS == Logits::kEvictInLds) {
     if (row < rows) scores = reinterpret_cast<float*>(lds + Lds<D, WAVES, KH>::kBytes) + row * strip_pitch(ev.n);
   } else if constexpr (LOGITS != Logits::kNone) {
-    if (row < rows) scores = a.scores + (static_cast<int64_t>(blockIdx.y) * dm.Hq + h) * a.score_pitch;
+    if (row < rows) scores = a.scores + (static_cast<int64_t>(blockIdx.z) * dm.Hq + g * dm.G + row) * a.score_pitch;  // nodes == 1
   }
 
+  EvictAhead<64 * WAVES> ahead;
+  if constexpr (LOGITS == Logits::kEvict || LOGITS == Logits::kEvictInLds) ahead.ask(ev, b, l, g);
+  bool real = true;  // is there a node at this lane's row?
   auto over_the_keys = [&]<bool CAREFUL>() {
     int at_lane = lane;
     asm volatile("" : "+v"(at_lane));  // what follows from it is formed anew by the second pass: kept for it, it cost the first registers
     const int at_col = at_lane % 32, at_grp = at_lane / 32;
-    const int at_row = min((row_group * kBlocks + wu / KH) * 32 + at_col, rows - 1), at_t = at_row % nodes;
-    uint64_t word = a.words != nullptr ? a.words[b * a.words_sb + at_t] : 1;
+    const int at_row = min((row_group * kBlocks + wu / KH) * 32 + at_col, rows - 1);
+    const int head = a.by_nodes.quotient(at_row), node = at_row - head * nodes;
+    uint64_t word = a.words != nullptr ? a.words[b * a.words_sb + node] : 1;
+    real = word >> node & 1;
     if (nodes < 64) word &= (uint64_t{1} << nodes) - 1;
     // per-lane LDS read offsets inside a tile, swizzle included
     uint32_t k_off[T::kKk], v_off[2 * T::kOut];
@@ -266,7 +269,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
 
     bf16x8 q_op[T::kKk];
     auto load_queries = [&] {  // while the first keys are on their way; what is asked for later is counted from here
-      const uint16_t* qp = row_ptr<uint16_t>(a.q, b, l, g * dm.G + at_row / nodes, at_t) + 8 * at_grp;
+      const uint16_t* qp = row_ptr<uint16_t>(a.q, b, l, g * dm.G + head, node) + 8 * at_grp;
 #pragma unroll
       for (int kk = 0; kk < T::kKk; ++kk) {
         Pack8 x;
@@ -292,15 +295,15 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
     };
     if constexpr (kPrivate) {
       // key tiles of this workgroup's range, dealt to its waves in turn
-      const int tiles = (n + 31) / 32, per = (tiles + key_splits - 1) / key_splits;
-      const int end = min(tiles, (sp + 1) * per);
+      const int tiles = (n + 31) / 32, per = (tiles + a.splits - 1) / a.splits;
+      const int end = min(tiles, (at.sp + 1) * per);
       char* const mine = lds + wu * T::kWaveLdsBytes;  // [buffer][K | V][tile]
       const uint32_t mine_at = lds_at + wu * T::kWaveLdsBytes;
       auto fill_tile = [&](int x, int buf) {
         char* k_t = mine + buf * 2 * kTileBytes;
         fill(x * 32, 0, 32 / kR, k_t, k_t + kTileBytes);
       };
-      int x = sp * per + wu;
+      int x = at.sp * per + wu;
       if (x < end) fill_tile(x, 0);
       load_queries();
       for (int it = 0; x < end; x += WAVES, ++it) {
@@ -319,8 +322,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
       constexpr int kSub = kStageKeys / 32, kStageBytes = 2 * kSub * kTileBytes, kGroups = kStageKeys / kR / WAVES;
       constexpr int kLoads = 2 * kGroups;  // of a wave and stage, at least (the stage behind the cache's last row takes more)
       static_assert(kGroups >= 1 && kSub % KH == 0);
-      const int stages = (n + kStageKeys - 1) / kStageKeys, per = (stages + key_splits - 1) / key_splits;
-      const int begin = sp * per, end = min(stages, begin + per);
+      const int stages = (n + kStageKeys - 1) / kStageKeys, per = (stages + a.splits - 1) / a.splits;
+      const int begin = at.sp * per, end = min(stages, begin + per);
       auto fill_stage = [&](int x) {
         char* k_t = lds + (x - begin) % kStages * kStageBytes;
         fill(x * kStageKeys, wu * kGroups, kGroups, k_t, k_t + kSub * kTileBytes);
@@ -348,22 +351,21 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
     }
   };
   over_the_keys.template operator()<false>();
-  bool finite = true;
+  float zero = 0.f;
 #pragma unroll
   for (int r = 0; r < T::kOut; ++r)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) finite &= fabsf(c.o[r][i]) < INFINITY;
-  const bool real = a.words == nullptr || (a.words[b * a.words_sb + t] >> t & 1);
-  if (!__syncthreads_and(finite || row >= rows || !real)) over_the_keys.template operator()<true>();
+    for (int i = 0; i < 16; ++i) zero = fmaf(c.o[r][i], 0.f, zero);
+  if (!__syncthreads_and(zero == 0.f || row >= rows || !real)) over_the_keys.template operator()<true>();
 
   // ---- the waves of a block of rows join through LDS (the tiles have been read when every wave is here) ----
   constexpr int kPitch = D + 4;
   const float l_row = c.l + __shfl_xor(c.l, 32, 64);
   __syncthreads();
   float* const o_s = reinterpret_cast<float*>(lds);                                       // [wave][32 rows][kPitch]
-  float2* const ml_s = reinterpret_cast<float2*>(lds + Lds<D, WAVES, KH>::kRows);  // [wave][32]
+  WaveRow* const rows_s = reinterpret_cast<WaveRow*>(lds + Lds<D, WAVES, KH>::kRows);  // [wave][32]
   if (row < rows) {
-    if (grp == 0) ml_s[wu * 32 + col] = make_float2(c.m, l_row);
+    if (grp == 0) rows_s[wu * 32 + col] = WaveRow{c.m, l_row, real, 0};
 #pragma unroll
     for (int r = 0; r < T::kOut; ++r)
 #pragma unroll
@@ -377,17 +379,18 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
   __syncthreads();
   const int first = row_group * kBlocks * 32, here = min(kBlocks * 32, rows - first);
   if constexpr (LOGITS == Logits::kNone || LOGITS == Logits::kKept) {
-    join_waves<uint16_t, D, WAVES, KH>(a, o_s, ml_s, g, first, here, sp);
+    join_waves<uint16_t, D, WAVES, KH>(a, o_s, rows_s, b, l, g, first, here, at.sp);
   } else {
     float* const lse2 = reinterpret_cast<float*>(lds + Lds<D, WAVES, KH>::kJoin);
-    join_waves<uint16_t, D, WAVES, KH>(a, o_s, ml_s, g, first, here, sp, lse2);
+    join_waves<uint16_t, D, WAVES, KH>(a, o_s, rows_s, b, l, g, first, here, at.sp, lse2);
     __syncthreads();
-    Candidate* const scratch = reinterpret_cast<Candidate*>(lse2 + 32);
+    EvictLds<64 * WAVES>& scratch = *reinterpret_cast<EvictLds<64 * WAVES>*>(lse2 + 32);
     if constexpr (LOGITS == Logits::kEvictInLds)
-      evict_unit<64 * WAVES>(ev, b, l, g, reinterpret_cast<const float*>(lds + Lds<D, WAVES, KH>::kBytes), strip_pitch(ev.n), lse2, scratch);
+      evict_unit<64 * WAVES>(ev, b, l, g, reinterpret_cast<const float*>(lds + Lds<D, WAVES, KH>::kBytes), strip_pitch(ev.n), lse2, ahead,
+                             scratch);
     else
-      evict_unit<64 * WAVES>(ev, b, l, g, a.scores + (static_cast<int64_t>(blockIdx.y) * dm.Hq + g * dm.G) * a.score_pitch, a.score_pitch,
-                             lse2, scratch);
+      evict_unit<64 * WAVES>(ev, b, l, g, a.scores + (static_cast<int64_t>(blockIdx.z) * dm.Hq + g * dm.G) * a.score_pitch, a.score_pitch,
+                             lse2, ahead, scratch);
   }
 }
 
@@ -399,7 +402,7 @@ hipError_t launch(const FewRows& a, const EvictStep& ev, int row_groups, hipStre
   const auto kernel = few_rows_kernel<D, WAVES, KH, PARTS, LOGITS>;
   const hipError_t e = raise_lds_limit(limit, reinterpret_cast<const void*>(kernel), LOGITS == Logits::kEvictInLds ? kLdsOfUnit - kLdsOfVote : L::kBytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(row_groups * a.dm.Hkv * a.splits, a.dm.B * a.dm.L), dim3(64 * WAVES), L::kBytes + strip, st, a, ev);
+  hipLaunchKernelGGL(kernel, dim3(row_groups * a.splits, a.dm.Hkv, a.dm.B * a.dm.L), dim3(64 * WAVES), L::kBytes + strip, st, a, ev);
   return hipGetLastError();
 }
 template <int D>

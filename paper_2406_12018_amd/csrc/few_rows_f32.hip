@@ -13,8 +13,8 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 constexpr int kWaves = 4;
 template <int D>
 struct Lds {
-  static constexpr int kRows = kWaves * 32 * (D + 4) * 4, kJoin = kRows + kWaves * 32 * 8;  // o_s, ml_s
-  static constexpr int kBytes = kJoin + 32 * 4 + (kWaves + 1) * 8;                          // lse2, Candidates
+  static constexpr int kRows = kWaves * 32 * (D + 4) * 4, kJoin = kRows + kWaves * 32 * 16;  // o_s, rows_s
+  static constexpr int kBytes = kJoin + 32 * 4 + sizeof(EvictLds<64 * kWaves>);             // lse2
 };
 
 // What a tile's V is read as: a lane has kOut consecutive elements of a row.
@@ -25,7 +25,7 @@ struct Values {
 };
 
 enum class Logits { kNone, kKept, kEvict };
-// grid: (row groups * Hkv * key ranges, B * L)
+// grid: (row groups * key ranges, Hkv, B * L)
 template <int D, Logits LOGITS>
 __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, EvictStep ev) {
   constexpr int kOut = D / 32, kPieces = D / 8;
@@ -33,14 +33,16 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
   const Dims& dm = a.dm;
   const int lane = threadIdx.x % 64, col = lane % 32, grp = lane / 32;
   const int wu = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int sp = blockIdx.x % a.splits, g = blockIdx.x / a.splits % dm.Hkv, row_group = blockIdx.x / a.splits / dm.Hkv;
-  const int b = blockIdx.y / dm.L, l = blockIdx.y % dm.L;
+  const Place place(a);
+  const int b = place.b, l = place.l, g = place.g, row_group = place.row_group;
   const int nodes = a.ks.c, rows = dm.G * nodes;
   const int n_c = a.lens != nullptr ? min(max(a.lens[b], 0), a.ks.n_c) : a.ks.n_c;
   const int n = n_c + nodes;
-  const int row = row_group * 32 + col, h = g * dm.G + min(row, rows - 1) / nodes, t = min(row, rows - 1) % nodes;
+  const int row = row_group * 32 + col, head = a.by_nodes.quotient(min(row, rows - 1)), t = min(row, rows - 1) - head * nodes;
+  const int h = g * dm.G + head;
   uint64_t word = a.words != nullptr ? a.words[b * a.words_sb + t] : 1;
   if (nodes < 64) word &= (uint64_t{1} << nodes) - 1;
+  const bool real = word >> t & 1;
   const float c2 = dm.scale * kLog2e;
 
   // Elements 8 i + 4 grp .. + 3 of a row are this lane's part of its products, of a query and of a key alike.
@@ -65,10 +67,10 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
     for (int i = 0; i < 16; ++i) o[r][i] = 0.f;
   float* scores = nullptr;
   if constexpr (LOGITS != Logits::kNone)
-    if (row < rows) scores = a.scores + (static_cast<int64_t>(blockIdx.y) * dm.Hq + h) * a.score_pitch;
+    if (row < rows) scores = a.scores + (static_cast<int64_t>(blockIdx.z) * dm.Hq + h) * a.score_pitch;
 
-  const int tiles = (n + 31) / 32, per = (tiles + a.splits - 1) / a.splits, end = min(tiles, (sp + 1) * per);
-  int x = sp * per + wu;
+  const int tiles = (n + 31) / 32, per = (tiles + a.splits - 1) / a.splits, end = min(tiles, (place.sp + 1) * per);
+  int x = place.sp * per + wu;
   if (x < end) load_keys(x);
   for (; x < end; x += kWaves) {
     const int j0 = 32 * x, own = j0 - n_c;
@@ -164,9 +166,9 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
 
   sum += __shfl_xor(sum, 32, 64);
   float* const o_s = reinterpret_cast<float*>(lds);
-  float2* const ml_s = reinterpret_cast<float2*>(lds + Lds<D>::kRows);
+  WaveRow* const rows_s = reinterpret_cast<WaveRow*>(lds + Lds<D>::kRows);
   if (row < rows) {
-    if (grp == 0) ml_s[wu * 32 + col] = make_float2(m, sum);
+    if (grp == 0) rows_s[wu * 32 + col] = WaveRow{m, sum, real, 0};
     float* const at = o_s + (wu * 32 + col) * (D + 4);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -176,13 +178,15 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
   __syncthreads();
   const int here = min(32, rows - row_group * 32);
   if constexpr (LOGITS == Logits::kEvict) {
+    EvictAhead<64 * kWaves> ahead;
+    ahead.ask(ev, b, l, g);
     float* const lse2 = reinterpret_cast<float*>(lds + Lds<D>::kJoin);
-    join_waves<float, D, kWaves, kWaves>(a, o_s, ml_s, g, 0, here, sp, lse2);
+    join_waves<float, D, kWaves, kWaves>(a, o_s, rows_s, b, l, g, 0, here, place.sp, lse2);
     __syncthreads();
-    evict_unit<64 * kWaves>(ev, b, l, g, a.scores + (static_cast<int64_t>(blockIdx.y) * dm.Hq + g * dm.G) * a.score_pitch, a.score_pitch, lse2,
-                            reinterpret_cast<Candidate*>(lse2 + 32));
+    evict_unit<64 * kWaves>(ev, b, l, g, a.scores + (static_cast<int64_t>(blockIdx.z) * dm.Hq + g * dm.G) * a.score_pitch, a.score_pitch, lse2,
+                            ahead, *reinterpret_cast<EvictLds<64 * kWaves>*>(lse2 + 32));
   } else {
-    join_waves<float, D, kWaves, kWaves>(a, o_s, ml_s, g, row_group * 32, here, sp);
+    join_waves<float, D, kWaves, kWaves>(a, o_s, rows_s, b, l, g, row_group * 32, here, place.sp);
   }
 }
 
@@ -192,7 +196,7 @@ hipError_t launch(const FewRows& a, const FewRowsPlan& p, const EvictStep& ev, h
   const auto kernel = few_rows_f32_kernel<D, LOGITS>;
   const hipError_t e = raise_lds_limit(limit, reinterpret_cast<const void*>(kernel), Lds<D>::kBytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(p.row_groups * a.dm.Hkv * a.splits, a.dm.B * a.dm.L), dim3(64 * kWaves), Lds<D>::kBytes, st, a, ev);
+  hipLaunchKernelGGL(kernel, dim3(p.row_groups * a.splits, a.dm.Hkv, a.dm.B * a.dm.L), dim3(64 * kWaves), Lds<D>::kBytes, st, a, ev);
   return hipGetLastError();
 }
 template <int D>

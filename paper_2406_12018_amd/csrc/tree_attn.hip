@@ -14,10 +14,12 @@ __global__ __launch_bounds__(256) void join_ranges_kernel(FewRows a) {
   const Dims& dm = a.dm;
   const int nodes = a.ks.c, e = blockIdx.x * 256 + threadIdx.x;
   if (e >= dm.Hq * nodes * (D / 4)) return;
-  const int d = e % (D / 4) * 4, r = e / (D / 4);
+  const int d = e % (D / 4) * 4, r = e / (D / 4), h = a.by_nodes.quotient(r), t = r - h * nodes;
+  const int b = a.by_layers.quotient(blockIdx.y), l = blockIdx.y - b * dm.L;
   const int64_t row = static_cast<int64_t>(blockIdx.y) * dm.Hq * nodes + r;
+  const bool real = is_node(a, b, t);
   RowParts p = join_ranges<D>(a, row, d);
-  finish_row<E>(a, blockIdx.y / dm.L, blockIdx.y % dm.L, r / nodes, r % nodes, row, d, p);
+  finish_row<E>(a, b, l, h, t, row, d, p, real);
 }
 
 constexpr int kMostSplits = 64;
@@ -61,6 +63,9 @@ FewRowsPlan plan_for(int dtype, const Dims& dm, int nodes, int most_keys, bool l
 
 hipError_t launch_main(int dtype, FewRows& a, const FewRowsPlan& p, const EvictStep* ev, hipStream_t st) {
   a.splits = p.splits;
+  a.by_splits = fast_div(p.splits);
+  a.by_layers = fast_div(a.dm.L);
+  a.by_nodes = fast_div(a.ks.c);
   a.part_o = nullptr;
   if (p.splits > 1 || (ev != nullptr && !p.evicts)) {
     const size_t rows = static_cast<size_t>(p.splits) * a.dm.B * a.dm.L * a.dm.Hq * a.ks.c;
