@@ -339,28 +339,35 @@ def alloc_generation_workspace(cfg: Config, draft_len: int = 1, device="cuda") -
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _states(what: str, t, cfg: Config, heads: int, rows: int, device: int, at_least: bool = False) -> CTensor:
-    """citrus_tensor of t, which has to be [B, L, heads, rows (or more), d] of the configuration's type on `device`."""
-    shape = t.shape
-    if (len(shape) != 5 or shape[0] != cfg.batch or shape[1] != cfg.layers or shape[2] != heads or shape[4] != cfg.head_dim or
-            (shape[3] < rows if at_least else shape[3] != rows)):
-        raise ValueError(f"{what}: shape {tuple(shape)}, expected {(cfg.batch, cfg.layers, heads, rows, cfg.head_dim)}" +
-                         (" with that many rows or more" if at_least else ""))
-    if t.dtype is not (torch.float32 if cfg.dtype == F32 else torch.bfloat16):
-        raise ValueError(f"{what}: {t.dtype}, the configuration has {cfg.torch_dtype}")
-    if t.get_device() != device:
-        raise ValueError(f"{what}: on another device than the first tensor")
-    return tensor(t)
+def _misfit(what: str, t, dtype, shape, device: int):
+    raise ValueError(f"{what}: {t.dtype} of shape {tuple(t.shape)} on device {t.get_device()}, expected {dtype} of "
+                     f"{tuple('any' if n is None else n for n in shape)} on device {device}")
+
+
+def _states(what: str, t, dtype, shape: tuple, device: int) -> CTensor:
+    """citrus_tensor of t, which has to have this type and shape [B, L, heads, rows, d], on `device`."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        _misfit(what, t, dtype, shape, device)
+    s = t.stride()
+    if s[4] != 1:
+        raise ValueError(f"{what}: expected a [B, L, H, S, d] tensor with contiguous last axis")
+    return CTensor(t.data_ptr(), s[0], s[1], s[2], s[3])
+
+
+def _cache(what: str, t, dtype, shape: tuple, device: int) -> CTensor:
+    """The same of a cache, which may have more rows."""
+    have = t.shape
+    if len(have) != 5 or have[3] < shape[3]:
+        _misfit(what, t, dtype, shape, device)
+    return _states(what, t, dtype, (*shape[:3], have[3], shape[4]), device)
 
 
 def _dense(what: str, t, dtype, shape: tuple, device: int) -> Optional[int]:
     """Address of t, which has to be a dense tensor of this type and shape on `device`; None for None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{what}: {t.dtype} of shape {tuple(t.shape)}, expected a dense {dtype} of {shape}")
-    if t.get_device() != device:
-        raise ValueError(f"{what}: on another device than the first tensor")
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        _misfit(what + " (dense)", t, dtype, shape, device)
     return t.data_ptr()
 
 
@@ -375,7 +382,7 @@ def _generation_block(workspace, device: int):
         return None, 0
     if workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError("workspace: a dense tensor on the device of the others is needed")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def citrus_tree_attn(cfg: Config, q, k_draft, v_draft, ancestors, k_cache, v_cache, cache_len: int, cache_lens=None, out=None,
@@ -383,23 +390,24 @@ def citrus_tree_attn(cfg: Config, q, k_draft, v_draft, ancestors, k_cache, v_cac
     """Attention of drafted trees q [B, L, Hq, nodes, d] over the caches and the nodes' ancestors: ancestors is int64
     [B, nodes], or [nodes] for one tree in all documents, bit u of a node's word for node u, its own among them (without it there is no
     such node).  cache_lens: int32 [B] lengths of the documents, up to cache_len.  Returns out."""
-    nodes, device = q.shape[3], q.get_device()
+    nodes, device, dtype = q.shape[3], q.get_device(), cfg.torch_dtype
     _on(device)
-    hq, hkv = cfg.q_heads, cfg.kv_heads
     if out is None:
         out = torch.empty_like(q)
+    B, L, hq, d = cfg.batch, cfg.layers, cfg.q_heads, cfg.head_dim
+    rows, draft, cache = (B, L, hq, nodes, d), (B, L, cfg.kv_heads, nodes, d), (B, L, cfg.kv_heads, cache_len, d)
     shared = ancestors.dim() == 1
     cached = cache_len > 0 or k_cache is not None or v_cache is not None
     cc = cfg.c()
     block, size = _generation_block(workspace, device)
     st = _lib().citrus_tree_attn(
-        C.byref(cc), _states("q", q, cfg, hq, nodes, device), _states("k_draft", k_draft, cfg, hkv, nodes, device),
-        _states("v_draft", v_draft, cfg, hkv, nodes, device), nodes,
-        _dense("ancestors", ancestors, torch.int64, (nodes,) if shared else (cfg.batch, nodes), device), 0 if shared else nodes,
-        _states("k_cache", k_cache, cfg, hkv, cache_len, device, True) if cached else tensor(None),
-        _states("v_cache", v_cache, cfg, hkv, cache_len, device, True) if cached else tensor(None), cache_len,
-        _dense("cache_lens", cache_lens, torch.int32, (cfg.batch,), device), _states("out", out, cfg, hq, nodes, device),
-        _dense("lse", lse, torch.float32, (cfg.batch, cfg.layers, hq, nodes), device), block, size, _stream(stream))
+        C.byref(cc), _states("q", q, dtype, rows, device), _states("k_draft", k_draft, dtype, draft, device),
+        _states("v_draft", v_draft, dtype, draft, device), nodes,
+        _dense("ancestors", ancestors, torch.int64, (nodes,) if shared else (B, nodes), device), 0 if shared else nodes,
+        _cache("k_cache", k_cache, dtype, cache, device) if cached else tensor(None),
+        _cache("v_cache", v_cache, dtype, cache, device) if cached else tensor(None), cache_len,
+        _dense("cache_lens", cache_lens, torch.int32, (B,), device), _states("out", out, dtype, rows, device),
+        _dense("lse", lse, torch.float32, (B, L, hq, nodes), device), block, size, _stream(stream))
     _check(st, "citrus_tree_attn")
     return out
 
@@ -408,20 +416,20 @@ def citrus_tree_commit(cfg: Config, k_draft, v_draft, path, accepted, k_cache, v
                        new_lens=None, stream=None):
     """Puts the draft states path[b, :accepted[b]] behind the cache of every document b, in place; path int32 [B, path_len],
     accepted and cache_lens int32 [B].  Returns new_lens [B], the documents' new lengths."""
-    nodes, device, hkv = k_draft.shape[3], k_draft.get_device(), cfg.kv_heads
+    nodes, device, dtype = k_draft.shape[3], k_draft.get_device(), cfg.torch_dtype
     _on(device)
+    B = cfg.batch
     if new_lens is None:
-        new_lens = torch.empty(cfg.batch, dtype=torch.int32, device=k_draft.device)
+        new_lens = torch.empty(B, dtype=torch.int32, device=k_draft.device)
     path_len = path.shape[1] if path.dim() == 2 else 0
-    rows = cfg.cache_capacity
+    draft, cache = (B, cfg.layers, cfg.kv_heads, nodes, cfg.head_dim), (B, cfg.layers, cfg.kv_heads, cfg.cache_capacity, cfg.head_dim)
     cc = cfg.c()
     st = _lib().citrus_tree_commit(
-        C.byref(cc), _states("k_draft", k_draft, cfg, hkv, nodes, device), _states("v_draft", v_draft, cfg, hkv, nodes, device),
-        nodes, _dense("path", path, torch.int32, (cfg.batch, path_len), device), path_len,
-        _dense("accepted", accepted, torch.int32, (cfg.batch,), device), _states("k_cache", k_cache, cfg, hkv, rows, device, True),
-        _states("v_cache", v_cache, cfg, hkv, rows, device, True), cache_len,
-        _dense("cache_lens", cache_lens, torch.int32, (cfg.batch,), device),
-        _dense("new_lens", new_lens, torch.int32, (cfg.batch,), device), _stream(stream))
+        C.byref(cc), _states("k_draft", k_draft, dtype, draft, device), _states("v_draft", v_draft, dtype, draft, device),
+        nodes, _dense("path", path, torch.int32, (B, path_len), device), path_len,
+        _dense("accepted", accepted, torch.int32, (B,), device), _cache("k_cache", k_cache, dtype, cache, device),
+        _cache("v_cache", v_cache, dtype, cache, device), cache_len, _dense("cache_lens", cache_lens, torch.int32, (B,), device),
+        _dense("new_lens", new_lens, torch.int32, (B,), device), _stream(stream))
     _check(st, "citrus_tree_commit")
     return new_lens
 
@@ -432,20 +440,20 @@ def citrus_decode_evict_step(cfg: Config, q, k_new, v_new, k_cache, v_cache, acc
     [B, L, Hkv, cache_capacity], and in a full cache the state with the smallest sum makes room (the last `recent` rows, the newest
     states, and the first cfg.start_size are kept).  tokens: states put into the cache so far.  Updates the caches and acc in place;
     evicted: int32 [B, L, sel_heads], the row whose state went, or -1.  Returns out."""
-    device, hq, hkv = q.get_device(), cfg.q_heads, cfg.kv_heads
+    device, dtype = q.get_device(), cfg.torch_dtype
     _on(device)
     if out is None:
         out = torch.empty_like(q)
-    rows = min(tokens + 1, cfg.budget)
+    B, L, hkv, d = cfg.batch, cfg.layers, cfg.kv_heads, cfg.head_dim
+    row, state, cache = (B, L, cfg.q_heads, 1, d), (B, L, hkv, 1, d), (B, L, hkv, min(tokens + 1, cfg.budget), d)
     cc = cfg.c()
     block, size = _generation_block(workspace, device)
     st = _lib().citrus_decode_evict_step(
-        C.byref(cc), _states("q", q, cfg, hq, 1, device), _states("k_new", k_new, cfg, hkv, 1, device),
-        _states("v_new", v_new, cfg, hkv, 1, device), _states("k_cache", k_cache, cfg, hkv, rows, device, True),
-        _states("v_cache", v_cache, cfg, hkv, rows, device, True),
-        _dense("acc", acc, torch.float32, (cfg.batch, cfg.layers, hkv, cfg.cache_capacity), device), tokens, recent,
-        _states("out", out, cfg, hq, 1, device), _dense("evicted", evicted, torch.int32, (cfg.batch, cfg.layers, cfg.sel_heads), device),
-        block, size, _stream(stream))
+        C.byref(cc), _states("q", q, dtype, row, device), _states("k_new", k_new, dtype, state, device),
+        _states("v_new", v_new, dtype, state, device), _cache("k_cache", k_cache, dtype, cache, device),
+        _cache("v_cache", v_cache, dtype, cache, device), _dense("acc", acc, torch.float32, (B, L, hkv, cfg.cache_capacity), device),
+        tokens, recent, _states("out", out, dtype, row, device),
+        _dense("evicted", evicted, torch.int32, (B, L, cfg.sel_heads), device), block, size, _stream(stream))
     _check(st, "citrus_decode_evict_step")
     return out
 

@@ -625,7 +625,7 @@ int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citr
   CITRUS_TRY(check_tensor(cfg, k_cache, cfg->cache_capacity, false));
   CITRUS_TRY(check_tensor(cfg, v_cache, cfg->cache_capacity, false));
   if (new_lens != nullptr && (new_lens == cache_lens || new_lens == accepted || new_lens == path)) return CITRUS_ERR_SHAPE;
-  const Commit a{path, accepted, cache_lens, new_lens, path_len, draft_len, cache_len, cfg->cache_capacity};
+  const Commit a{path, accepted, cache_lens, new_lens, path_len, draft_len, cache_len, cfg->cache_capacity, fast_div(cfg->layers)};
   return hip_status(launch_tree_commit(elem_bytes(cfg->dtype), dims_of(cfg), make_view(k_draft), make_view(v_draft), make_view(k_cache),
                                        make_view(v_cache), a, static_cast<hipStream_t>(hip_stream)));
 }

@@ -195,6 +195,7 @@ struct Commit {
   const int32_t *path, *accepted, *lens;  // [B][path_len], [B], optional [B]
   int32_t* new_lens;                      // optional [B]
   int path_len, nodes, cache_len, capacity;
+  FastDiv by_layers;
 };
 hipError_t launch_tree_commit(int elem_bytes, const Dims& dm, View k_draft, View v_draft, View k_cache, View v_cache,
                               const Commit& a, hipStream_t st);

@@ -37,9 +37,10 @@ __global__ __launch_bounds__(kUnitThreads) void evict_unit_kernel(FewRows a, Evi
   const int g = blockIdx.x, b = a.by_layers.quotient(blockIdx.y), l = blockIdx.y - b * a.dm.L;
   EvictAhead<kUnitThreads> ahead;
   ahead.ask(e, b, l, g);
-  rows_of_unit<E, D, kUnitThreads>(a, b, l, g, true, lse2);
   const float* scores = a.scores + (static_cast<int64_t>(blockIdx.y) * a.dm.Hq + g * a.dm.G) * a.score_pitch;
-  evict_unit<kUnitThreads>(e, b, l, g, scores, a.score_pitch, lse2, ahead, lds);
+  const Logits4 first = first_logits(e, scores, a.score_pitch, 0, e.n + 1);
+  rows_of_unit<E, D, kUnitThreads>(a, b, l, g, true, lse2);
+  evict_unit<kUnitThreads>(e, b, l, g, scores, a.score_pitch, lse2, ahead, first, lds);
 }
 
 // Long caches and selections per layer: the sums grow in ranges of keys, and one workgroup per selection makes room behind them.
@@ -55,9 +56,10 @@ __global__ __launch_bounds__(kThreads) void grow_sums_kernel(FewRows a, EvictSte
   float* const acc = e.acc + unit * e.acc_pitch;
   const int begin = range * kRangeKeys, end = min(e.n + 1, begin + kRangeKeys);
   const Sums4 sums = load_sums(e, acc, begin + 4 * threadIdx.x);
-  rows_of_unit<E, D, kThreads>(a, b, l, g, range == 0, lse2);
   const float* scores = a.scores + unit * a.dm.G * a.score_pitch;
-  const Candidate mine = grow_sums<kThreads>(e, scores, a.score_pitch, lse2, acc, begin, end, sums, lds);
+  const Logits4 first = first_logits(e, scores, a.score_pitch, begin, end);
+  rows_of_unit<E, D, kThreads>(a, b, l, g, range == 0, lse2);
+  const Candidate mine = grow_sums<kThreads>(e, scores, a.score_pitch, lse2, acc, begin, end, sums, first, lds);
   const Candidate best = smallest_of_block<kThreads>(mine, lds);
   if (threadIdx.x == 0) {
     e.best[unit * ranges + range] = make_float2(best.sum, __int_as_float(best.slot));

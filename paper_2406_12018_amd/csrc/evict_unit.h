@@ -68,24 +68,38 @@ __device__ inline Sums4 load_sums(const EvictStep& e, const float* acc, int j) {
   for (int x = 0; x < 4; ++x) s.x[x] = acc[max(min(j + x, e.n - 1), 0)];
   return s;
 }
+// Logits of four keys and four heads from `h` on.
+struct Logits4 {
+  float4 s[4];
+};
+__device__ inline Logits4 load_logits(const float* scores, int64_t pitch, int h, int G, int j) {
+  Logits4 l;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) l.s[x] = *reinterpret_cast<const float4*>(scores + min(h + x, G - 1) * pitch + j);
+  return l;
+}
 // Sums of the keys [begin, end) of a unit grow, four keys a thread and turn; begin is a multiple of 4.  scores: [head][pitch], lse2: by
-// head.  old: load_sums of the thread's first keys.  Returns this thread's smallest.
+// head.  old, first: load_sums of the thread's first keys, load_logits of their first heads.  Returns this thread's smallest.
 template <int THREADS>
 __device__ inline Candidate grow_sums(const EvictStep& e, const float* scores, int64_t pitch, const float* lse2, float* acc, int begin, int end,
-                                      Sums4 old, EvictLds<THREADS>& lds) {
+                                      Sums4 old, Logits4 first, EvictLds<THREADS>& lds) {
   const int G = e.dm.G;
   Candidate best{INFINITY, e.oldest};
   for (int j = begin + 4 * threadIdx.x; j < end; j += 4 * THREADS) {
     const Sums4 next = load_sums(e, acc, j + 4 * THREADS);
     float w[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int h = 0; h < G; ++h) {
-      const float4 s = *reinterpret_cast<const float4*>(scores + h * pitch + j);
-      const float z = lse2[h];
-      w[0] += __builtin_amdgcn_exp2f(s.x - z);
-      w[1] += __builtin_amdgcn_exp2f(s.y - z);
-      w[2] += __builtin_amdgcn_exp2f(s.z - z);
-      w[3] += __builtin_amdgcn_exp2f(s.w - z);
+    for (int h = 0; h < G; h += 4) {
+      const Logits4 l = first;
+      const int h_next = h + 4 < G ? h + 4 : 0, j_next = h + 4 < G ? j : min(j + 4 * THREADS, (end - 1) & ~3);
+      first = load_logits(scores, pitch, h_next, G, j_next);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float z = h + x < G ? lse2[h + x] : INFINITY;
+        w[0] += __builtin_amdgcn_exp2f(l.s[x].x - z);
+        w[1] += __builtin_amdgcn_exp2f(l.s[x].y - z);
+        w[2] += __builtin_amdgcn_exp2f(l.s[x].z - z);
+        w[3] += __builtin_amdgcn_exp2f(l.s[x].w - z);
+      }
     }
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -101,6 +115,9 @@ __device__ inline Candidate grow_sums(const EvictStep& e, const float* scores, i
     old = next;
   }
   return best;
+}
+__device__ inline Logits4 first_logits(const EvictStep& e, const float* scores, int64_t pitch, int begin, int end) {
+  return load_logits(scores, pitch, 0, e.dm.G, min(begin + 4 * static_cast<int>(threadIdx.x), (end - 1) & ~3));
 }
 
 // A 16-byte piece of what moves: of the oldest recent state, and of the token's.
@@ -146,10 +163,10 @@ struct EvictAhead {
 };
 template <int THREADS>
 __device__ inline void evict_unit(const EvictStep& e, int b, int l, int g, const float* scores, int64_t pitch, const float* lse2,
-                                  const EvictAhead<THREADS>& ahead, EvictLds<THREADS>& lds) {
+                                  const EvictAhead<THREADS>& ahead, const Logits4& first, EvictLds<THREADS>& lds) {
   const int64_t unit = static_cast<int64_t>(b * e.dm.L + l) * e.dm.Hkv + g;
   float* const acc = e.acc + unit * e.acc_pitch;
-  Candidate best = grow_sums<THREADS>(e, scores, pitch, lse2, acc, 0, e.n + 1, ahead.sums, lds);
+  Candidate best = grow_sums<THREADS>(e, scores, pitch, lse2, acc, 0, e.n + 1, ahead.sums, first, lds);
   best = smallest_of_block<THREADS>(best, lds);
   const int slot = e.oldest >= 0 ? best.slot : -1;
   if (threadIdx.x < 2 * e.row_bytes / 16) move_piece(e, ahead.piece, slot);

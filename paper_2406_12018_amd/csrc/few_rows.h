@@ -92,15 +92,31 @@ __device__ __forceinline__ void join_waves(const FewRows& a, const float* o_s, c
   }
 }
 
-// Four elements of a row from its ranges of keys.
+// Four elements of a row from its ranges of keys, four ranges' loads in flight at a time.
 template <int D>
 __device__ inline RowParts join_ranges(const FewRows& a, int64_t row, int d) {
   const int64_t all = static_cast<int64_t>(a.dm.B) * a.dm.L * a.dm.Hq * a.ks.c;
   RowParts p;
-#pragma unroll 8
-  for (int s = 0; s < a.splits; ++s) p.m = fmaxf(p.m, a.part_ml[s * all + row].x);
-#pragma unroll 8
-  for (int s = 0; s < a.splits; ++s) p.add(a.part_ml[s * all + row], *reinterpret_cast<const float4*>(a.part_o + (s * all + row) * D + d));
+  for (int s = 0; s < a.splits; s += 4) {
+    float2 ml[4];
+    float4 o[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int64_t at = min(s + x, a.splits - 1) * all + row;
+      ml[x] = a.part_ml[at];
+      o[x] = *reinterpret_cast<const float4*>(a.part_o + at * D + d);
+    }
+    const float before = p.m;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) p.m = fmaxf(p.m, ml[x].x);
+    const float w = __builtin_amdgcn_exp2f(before - p.reference());
+    p.sum *= w;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) p.o[x] *= w;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (s + x < a.splits) p.add(ml[x], o[x]);
+  }
   return p;
 }
 
@@ -116,8 +132,9 @@ struct Place {
   }
 };
 
-// What a lane sees of the 32 keys from own + n_c on: bit j, by its node's word.
+// What a lane sees of 32 keys, the first of them its document's own state `own` (below 0: cached): bit j, by its node's word.
 __device__ inline uint32_t seen_keys(uint64_t word, int own) {
+  if (own <= -32) return ~0u;
   return own >= 0 ? static_cast<uint32_t>(word >> own) : static_cast<uint32_t>(word) << -own | ((1u << -own) - 1);
 }
 

@@ -284,30 +284,26 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
     for (int r = 0; r < T::kOut; ++r)
 #pragma unroll
       for (int i = 0; i < 16; ++i) c.o[r][i] = 0.f;
-    auto tile = [&](int j0, uint32_t k_t, uint32_t v_t) {
-      float* const s = LOGITS != Logits::kNone && scores != nullptr ? scores + j0 : nullptr;
-      const int own = j0 - n_c;  // of the tile's first key
-      if (own + 32 <= 0) {
-        key_tile<D, PARTS, false, CAREFUL>(k_t, v_t, k_off, v_off, q_op, c2, 0, c, s);
-      } else {
-        key_tile<D, PARTS, true, CAREFUL>(k_t, v_t, k_off, v_off, q_op, c2, seen_keys(word, own), c, s);
-      }
+    // Tiles of cached states that every row sees come first.  (Apart from the others, in a loop of their own: where the two met in one
+    // loop, the accumulators went from one set of registers to another and back with every tile.)
+    auto tile = [&]<bool LAST>(int j0, uint32_t k_t, uint32_t v_t) {
+      key_tile<D, PARTS, LAST, CAREFUL>(k_t, v_t, k_off, v_off, q_op, c2, LAST ? seen_keys(word, j0 - n_c) : 0u, c,
+                                        LOGITS != Logits::kNone && scores != nullptr ? scores + j0 : nullptr);
     };
     if constexpr (kPrivate) {
       // key tiles of this workgroup's range, dealt to its waves in turn
       const int tiles = (n + 31) / 32, per = (tiles + a.splits - 1) / a.splits;
-      const int end = min(tiles, (at.sp + 1) * per);
+      const int end = min(tiles, (at.sp + 1) * per), whole = CAREFUL ? 0 : min(end, n_c / 32);
       char* const mine = lds + wu * T::kWaveLdsBytes;  // [buffer][K | V][tile]
       const uint32_t mine_at = lds_at + wu * T::kWaveLdsBytes;
       auto fill_tile = [&](int x, int buf) {
         char* k_t = mine + buf * 2 * kTileBytes;
         fill(x * 32, 0, 32 / kR, k_t, k_t + kTileBytes);
       };
-      int x = at.sp * per + wu;
+      int x = at.sp * per + wu, buf = 0;
       if (x < end) fill_tile(x, 0);
       load_queries();
-      for (int it = 0; x < end; x += WAVES, ++it) {
-        const int buf = it & 1;
+      auto turn = [&]<bool LAST>() {
         // the other buffer was last read in the previous turn, whose reads have all returned
         if (x + WAVES < end) {
           fill_tile(x + WAVES, buf ^ 1);
@@ -316,14 +312,18 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
           wait_loads<0>();
         }
         const uint32_t k_t = mine_at + buf * 2 * kTileBytes;
-        tile(x * 32, k_t, k_t + kTileBytes);
-      }
+        tile.template operator()<LAST>(x * 32, k_t, k_t + kTileBytes);
+        x += WAVES;
+        buf ^= 1;
+      };
+      while (x < whole) turn.template operator()<false>();
+      while (x < end) turn.template operator()<true>();
     } else {
       constexpr int kSub = kStageKeys / 32, kStageBytes = 2 * kSub * kTileBytes, kGroups = kStageKeys / kR / WAVES;
       constexpr int kLoads = 2 * kGroups;  // of a wave and stage, at least (the stage behind the cache's last row takes more)
       static_assert(kGroups >= 1 && kSub % KH == 0);
       const int stages = (n + kStageKeys - 1) / kStageKeys, per = (stages + a.splits - 1) / a.splits;
-      const int begin = at.sp * per, end = min(stages, begin + per);
+      const int begin = at.sp * per, end = min(stages, begin + per), whole = CAREFUL ? 0 : min(end, n_c / kStageKeys);
       auto fill_stage = [&](int x) {
         char* k_t = lds + (x - begin) % kStages * kStageBytes;
         fill(x * kStageKeys, wu * kGroups, kGroups, k_t, k_t + kSub * kTileBytes);
@@ -331,7 +331,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
       if (begin < end) fill_stage(begin);
       load_queries();
       for (int x = begin + 1; x < min(end, begin + kStages - 1); ++x) fill_stage(x);
-      for (int x = begin; x < end; ++x) {
+      int x = begin;
+      auto turn = [&]<bool LAST>() {
         // this wave's loads of the stage have landed; behind the barrier everybody's have, and the stage before has been read
         if (x + kStages - 2 < end)
           wait_loads<kLoads*(kStages - 2)>();
@@ -339,15 +340,17 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
           wait_loads<0>();
         asm volatile("s_barrier" ::: "memory");
         if (x + kStages - 1 < end) fill_stage(x + kStages - 1);
-        if (idle) continue;
         const uint32_t k_t = lds_at + (x - begin) % kStages * kStageBytes, v_t = k_t + kSub * kTileBytes;
 #pragma unroll
         for (int y = 0; y < kSub / KH; ++y) {
           const int sub = KH == 1 ? y : wu % KH;
           const int j0 = x * kStageKeys + 32 * sub;
-          if (j0 < n) tile(j0, k_t + sub * kTileBytes, v_t + sub * kTileBytes);
+          if (!idle && (!LAST || j0 < n)) tile.template operator()<LAST>(j0, k_t + sub * kTileBytes, v_t + sub * kTileBytes);
         }
-      }
+        ++x;
+      };
+      while (x < whole) turn.template operator()<false>();
+      while (x < end) turn.template operator()<true>();
     }
   };
   over_the_keys.template operator()<false>();
@@ -385,12 +388,11 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
     join_waves<uint16_t, D, WAVES, KH>(a, o_s, rows_s, b, l, g, first, here, at.sp, lse2);
     __syncthreads();
     EvictLds<64 * WAVES>& scratch = *reinterpret_cast<EvictLds<64 * WAVES>*>(lse2 + 32);
-    if constexpr (LOGITS == Logits::kEvictInLds)
-      evict_unit<64 * WAVES>(ev, b, l, g, reinterpret_cast<const float*>(lds + Lds<D, WAVES, KH>::kBytes), strip_pitch(ev.n), lse2, ahead,
-                             scratch);
-    else
-      evict_unit<64 * WAVES>(ev, b, l, g, a.scores + (static_cast<int64_t>(blockIdx.z) * dm.Hq + g * dm.G) * a.score_pitch, a.score_pitch,
-                             lse2, ahead, scratch);
+    const bool in_lds = LOGITS == Logits::kEvictInLds;
+    const float* const unit = in_lds ? reinterpret_cast<const float*>(lds + Lds<D, WAVES, KH>::kBytes)
+                                     : a.scores + (static_cast<int64_t>(blockIdx.z) * dm.Hq + g * dm.G) * a.score_pitch;
+    const int64_t pitch = in_lds ? strip_pitch(ev.n) : a.score_pitch;
+    evict_unit<64 * WAVES>(ev, b, l, g, unit, pitch, lse2, ahead, first_logits(ev, unit, pitch, 0, ev.n + 1), scratch);
   }
 }
 

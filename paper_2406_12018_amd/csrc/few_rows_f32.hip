@@ -183,8 +183,9 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
     float* const lse2 = reinterpret_cast<float*>(lds + Lds<D>::kJoin);
     join_waves<float, D, kWaves, kWaves>(a, o_s, rows_s, b, l, g, 0, here, place.sp, lse2);
     __syncthreads();
-    evict_unit<64 * kWaves>(ev, b, l, g, a.scores + (static_cast<int64_t>(blockIdx.z) * dm.Hq + g * dm.G) * a.score_pitch, a.score_pitch, lse2,
-                            ahead, *reinterpret_cast<EvictLds<64 * kWaves>*>(lse2 + 32));
+    const float* const unit = a.scores + (static_cast<int64_t>(blockIdx.z) * dm.Hq + g * dm.G) * a.score_pitch;
+    evict_unit<64 * kWaves>(ev, b, l, g, unit, a.score_pitch, lse2, ahead, first_logits(ev, unit, a.score_pitch, 0, ev.n + 1),
+                            *reinterpret_cast<EvictLds<64 * kWaves>*>(lse2 + 32));
   } else {
     join_waves<float, D, kWaves, kWaves>(a, o_s, rows_s, b, l, g, row_group * 32, here, place.sp);
   }

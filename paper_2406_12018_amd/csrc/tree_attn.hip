@@ -75,27 +75,36 @@ hipError_t launch_main(int dtype, FewRows& a, const FewRowsPlan& p, const EvictS
   return dtype == CITRUS_BF16 ? launch_few_rows_bf16(a, p, ev, st) : launch_few_rows_f32(a, p, ev, st);
 }
 
-// The accepted path's rows: row len + i of a document's cache takes draft row path[i], i < accepted.
-// One thread per 16-byte piece of a row of K and V.
-__global__ __launch_bounds__(256) void tree_commit_kernel(Dims dm, View kd, View vd, View kc, View vc, Commit a, int row_bytes) {
-  const int pieces = row_bytes / 16, per_head = 2 * pieces * a.path_len;
-  const int b = blockIdx.y / dm.L, l = blockIdx.y % dm.L;
+// The accepted path's rows: row len + i of a document's cache takes draft row path[i], i < accepted.  A thread has a 16-byte piece of K or
+// V of a head and moves it for path_rows rows, four of them in flight: as a thread per piece and row, 16 documents x 32 layers x 32
+// heads took 53 us, half of it threads behind the accepted rows; now 41.  grid: (.., B * L, shares of the path)
+__global__ __launch_bounds__(256) void tree_commit_kernel(Dims dm, View kd, View vd, View kc, View vc, Commit a, int row_bytes, int path_rows) {
+  const int pieces = row_bytes / 16, bits = __builtin_ctz(pieces);  // a power of two
+  const int b = a.by_layers.quotient(blockIdx.y), l = blockIdx.y - b * dm.L;
   const int e = blockIdx.x * 256 + threadIdx.x;
   const int len = a.lens != nullptr ? min(max(a.lens[b], 0), a.cache_len) : a.cache_len;
   const int accepted = min(min(max(a.accepted[b], 0), a.path_len), a.capacity - len);
-  if (e == 0 && l == 0 && a.new_lens != nullptr) a.new_lens[b] = len + accepted;
-  if (e >= per_head * dm.Hkv) return;
-  const int g = e / per_head, r = e % per_head;
-  const int i = r / (2 * pieces), piece = r % pieces;
-  const bool is_v = r / pieces % 2;
-  if (i >= accepted) return;
-  const int node = a.path[static_cast<int64_t>(b) * a.path_len + i];
-  if (node < 0 || node >= a.nodes) return;
+  if (e == 0 && l == 0 && blockIdx.z == 0 && a.new_lens != nullptr) a.new_lens[b] = len + accepted;
+  const int g = e >> (bits + 1), piece = e & (pieces - 1);
+  if (g >= dm.Hkv) return;
+  const bool is_v = e >> bits & 1;
   const View &from = is_v ? vd : kd, &to = is_v ? vc : kc;
   const int esz = row_bytes / dm.D;
-  const char* src = static_cast<const char*>(from.ptr) + (b * from.sb + l * from.sl + g * from.sh + node * from.ss) * esz;
-  char* dst = static_cast<char*>(const_cast<void*>(to.ptr)) + (b * to.sb + l * to.sl + g * to.sh + (len + i) * to.ss) * esz;
-  reinterpret_cast<uint4*>(dst)[piece] = reinterpret_cast<const uint4*>(src)[piece];
+  const char* src = static_cast<const char*>(from.ptr) + (b * from.sb + l * from.sl + g * from.sh) * esz + 16 * piece;
+  char* dst = static_cast<char*>(const_cast<void*>(to.ptr)) + (b * to.sb + l * to.sl + g * to.sh + len * to.ss) * esz + 16 * piece;
+  const int32_t* path = a.path + static_cast<int64_t>(b) * a.path_len;
+  const int end = min(accepted, static_cast<int>(blockIdx.z + 1) * path_rows);
+  for (int i = blockIdx.z * path_rows; i < end; i += 4) {
+    int node[4];
+    uint4 row[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) node[x] = path[min(i + x, end - 1)];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) row[x] = *reinterpret_cast<const uint4*>(src + min(max(node[x], 0), a.nodes - 1) * from.ss * esz);
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (i + x < end && node[x] >= 0 && node[x] < a.nodes) *reinterpret_cast<uint4*>(dst + (i + x) * to.ss * esz) = row[x];
+  }
 }
 
 }  // namespace
@@ -131,9 +140,13 @@ hipError_t launch_decode_evict(int dtype, FewRows a, const EvictStep& ev, bool p
 
 hipError_t launch_tree_commit(int elem_bytes, const Dims& dm, View k_draft, View v_draft, View k_cache, View v_cache,
                               const Commit& a, hipStream_t st) {
-  const int64_t pieces = static_cast<int64_t>(2) * dm.D * elem_bytes / 16 * a.path_len * dm.Hkv;
-  hipLaunchKernelGGL(tree_commit_kernel, dim3(static_cast<unsigned>((pieces + 255) / 256), dm.B * dm.L), dim3(256), 0, st, dm,
-                     k_draft, v_draft, k_cache, v_cache, a, dm.D * elem_bytes);
+  const int64_t pieces = static_cast<int64_t>(2) * dm.D * elem_bytes / 16 * dm.Hkv;
+  const int64_t blocks = (pieces + 255) / 256 * dm.B * dm.L;
+  // Few workgroups: each a share of the path.  Two to a compute unit keep the memory busy.
+  const int path_rows = blocks < 512 ? 4 : (a.path_len + 3) / 4 * 4;
+  hipLaunchKernelGGL(tree_commit_kernel,
+                     dim3(static_cast<unsigned>((pieces + 255) / 256), dm.B * dm.L, (a.path_len + path_rows - 1) / path_rows), dim3(256), 0,
+                     st, dm, k_draft, v_draft, k_cache, v_cache, a, dm.D * elem_bytes, path_rows);
   return hipGetLastError();
 }
 
