@@ -155,8 +155,8 @@ struct FewRows {
   int64_t score_pitch;    // a multiple of 32
   float* workspace;       // few_rows_workspace_floats
   // of the launch: ranges of keys, and where their parts of the rows go (NULL: there is one, and it finishes its rows)
-  int splits;
-  FastDiv by_splits, by_layers, by_nodes;
+  int splits, row_groups, units;  // units: workgroups but for the row groups
+  FastDiv by_splits, by_layers, by_nodes, by_heads, by_eights;
   float2* part_ml;        // [range][B*L*Hq*c]: maximum (base 2), sum
   float* part_o;          // [range][B*L*Hq*c][D]
 };

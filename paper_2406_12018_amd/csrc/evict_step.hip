@@ -28,8 +28,8 @@ __device__ inline void rows_of_unit(const FewRows& a, int b, int l, int g, bool 
   __syncthreads();
 }
 
-// One workgroup per unit.  grid: (Hkv, B * L); LDS: G floats
-constexpr int kUnitThreads = 512;
+// One workgroup per unit.  grid: (Hkv, B * L); LDS: G floats.  At 4096 keys of one layer two launches in ranges take 13 us, this one 9.
+constexpr int kUnitThreads = 512, kUnitKeys = 8192;
 template <typename E, int D>
 __global__ __launch_bounds__(kUnitThreads) void evict_unit_kernel(FewRows a, EvictStep e) {
   extern __shared__ float lse2[];
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(kUnitThreads) void evict_unit_kernel(FewRows a, Evi
   EvictAhead<kUnitThreads> ahead;
   ahead.ask(e, b, l, g);
   const float* scores = a.scores + (static_cast<int64_t>(blockIdx.y) * a.dm.Hq + g * a.dm.G) * a.score_pitch;
-  const Logits4 first = first_logits(e, scores, a.score_pitch, 0, e.n + 1);
+  const TwoTurns first = first_turns<kUnitThreads>(e, scores, a.score_pitch, 0, e.n + 1);
   rows_of_unit<E, D, kUnitThreads>(a, b, l, g, true, lse2);
   evict_unit<kUnitThreads>(e, b, l, g, scores, a.score_pitch, lse2, ahead, first, lds);
 }
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(kThreads) void grow_sums_kernel(FewRows a, EvictSte
   const int begin = range * kRangeKeys, end = min(e.n + 1, begin + kRangeKeys);
   const Sums4 sums = load_sums(e, acc, begin + 4 * threadIdx.x);
   const float* scores = a.scores + unit * a.dm.G * a.score_pitch;
-  const Logits4 first = first_logits(e, scores, a.score_pitch, begin, end);
+  const TwoTurns first = first_turns<kThreads>(e, scores, a.score_pitch, begin, end);
   rows_of_unit<E, D, kThreads>(a, b, l, g, range == 0, lse2);
   const Candidate mine = grow_sums<kThreads>(e, scores, a.score_pitch, lse2, acc, begin, end, sums, first, lds);
   const Candidate best = smallest_of_block<kThreads>(mine, lds);
@@ -102,7 +102,7 @@ hipError_t launch(const FewRows& a, const EvictStep& e, bool per_layer, hipStrea
   const dim3 units(e.dm.Hkv, e.dm.B * e.dm.L);
   const size_t lds = e.dm.G * sizeof(float);
   const int ranges = evict_step_ranges(e.n);
-  if (!per_layer && ranges == 1) {
+  if (!per_layer && e.n < kUnitKeys) {
     hipLaunchKernelGGL((evict_unit_kernel<E, D>), units, dim3(kUnitThreads), lds, st, a, e);
     return hipGetLastError();
   }

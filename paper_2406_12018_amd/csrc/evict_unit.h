@@ -78,46 +78,64 @@ __device__ inline Logits4 load_logits(const float* scores, int64_t pitch, int h,
   for (int x = 0; x < 4; ++x) l.s[x] = *reinterpret_cast<const float4*>(scores + min(h + x, G - 1) * pitch + j);
   return l;
 }
-// Sums of the keys [begin, end) of a unit grow, four keys a thread and turn; begin is a multiple of 4.  scores: [head][pitch], lse2: by
-// head.  old, first: load_sums of the thread's first keys, load_logits of their first heads.  Returns this thread's smallest.
+// Sums of the keys [begin, end) of a unit grow, four keys and four heads a thread and turn, the logits two turns ahead; begin is a multiple
+// of 4.  scores: [head][pitch], lse2: by head.  old, first, second: load_sums of the thread's first keys, the logits of its first turns.
+// Returns this thread's smallest.
+struct Turn {
+  int j, h;
+  template <int THREADS>
+  __device__ Turn next(int G) const { return h + 4 < G ? Turn{j, h + 4} : Turn{j + 4 * THREADS, 0}; }
+  __device__ Logits4 logits(const float* scores, int64_t pitch, int G, int end) const {
+    return load_logits(scores, pitch, h, G, min(j, (end - 1) & ~3));
+  }
+};
+struct TwoTurns {
+  Logits4 first, second;
+};
+template <int THREADS>
+__device__ inline TwoTurns first_turns(const EvictStep& e, const float* scores, int64_t pitch, int begin, int end) {
+  const Turn t{begin + 4 * static_cast<int>(threadIdx.x), 0};
+  return TwoTurns{t.logits(scores, pitch, e.dm.G, end), t.next<THREADS>(e.dm.G).logits(scores, pitch, e.dm.G, end)};
+}
 template <int THREADS>
 __device__ inline Candidate grow_sums(const EvictStep& e, const float* scores, int64_t pitch, const float* lse2, float* acc, int begin, int end,
-                                      Sums4 old, Logits4 first, EvictLds<THREADS>& lds) {
+                                      Sums4 old, TwoTurns ahead, EvictLds<THREADS>& lds) {
   const int G = e.dm.G;
   Candidate best{INFINITY, e.oldest};
-  for (int j = begin + 4 * threadIdx.x; j < end; j += 4 * THREADS) {
-    const Sums4 next = load_sums(e, acc, j + 4 * THREADS);
-    float w[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int h = 0; h < G; h += 4) {
-      const Logits4 l = first;
-      const int h_next = h + 4 < G ? h + 4 : 0, j_next = h + 4 < G ? j : min(j + 4 * THREADS, (end - 1) & ~3);
-      first = load_logits(scores, pitch, h_next, G, j_next);
+  Sums4 next;
+  float w[4];
+  for (Turn t{begin + 4 * static_cast<int>(threadIdx.x), 0}; t.j < end; t = t.next<THREADS>(G)) {
+    const Logits4 l = ahead.first;
+    ahead.first = ahead.second;
+    ahead.second = t.next<THREADS>(G).template next<THREADS>(G).logits(scores, pitch, G, end);
+    if (t.h == 0) {
+      next = load_sums(e, acc, t.j + 4 * THREADS);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const float z = h + x < G ? lse2[h + x] : INFINITY;
-        w[0] += __builtin_amdgcn_exp2f(l.s[x].x - z);
-        w[1] += __builtin_amdgcn_exp2f(l.s[x].y - z);
-        w[2] += __builtin_amdgcn_exp2f(l.s[x].z - z);
-        w[3] += __builtin_amdgcn_exp2f(l.s[x].w - z);
-      }
+      for (int x = 0; x < 4; ++x) w[x] = 0.f;
     }
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      if (j + x < e.n) {
+      const float z = t.h + x < G ? lse2[t.h + x] : INFINITY;
+      w[0] += __builtin_amdgcn_exp2f(l.s[x].x - z);
+      w[1] += __builtin_amdgcn_exp2f(l.s[x].y - z);
+      w[2] += __builtin_amdgcn_exp2f(l.s[x].z - z);
+      w[3] += __builtin_amdgcn_exp2f(l.s[x].w - z);
+    }
+    if (t.h + 4 < G) continue;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      if (t.j + x < e.n) {
         const float sum = old.x[x] + w[x];
-        acc[j + x] = sum;
-        if (may_go(e, j + x)) best = smaller(best, Candidate{sum, j + x});
-        if (j + x == e.oldest) lds.oldest = sum;
-      } else if (j + x == e.n) {
+        acc[t.j + x] = sum;
+        if (may_go(e, t.j + x)) best = smaller(best, Candidate{sum, t.j + x});
+        if (t.j + x == e.oldest) lds.oldest = sum;
+      } else if (t.j + x == e.n) {
         lds.own = w[x];
       }
     }
     old = next;
   }
   return best;
-}
-__device__ inline Logits4 first_logits(const EvictStep& e, const float* scores, int64_t pitch, int begin, int end) {
-  return load_logits(scores, pitch, 0, e.dm.G, min(begin + 4 * static_cast<int>(threadIdx.x), (end - 1) & ~3));
 }
 
 // A 16-byte piece of what moves: of the oldest recent state, and of the token's.
@@ -163,7 +181,7 @@ struct EvictAhead {
 };
 template <int THREADS>
 __device__ inline void evict_unit(const EvictStep& e, int b, int l, int g, const float* scores, int64_t pitch, const float* lse2,
-                                  const EvictAhead<THREADS>& ahead, const Logits4& first, EvictLds<THREADS>& lds) {
+                                  const EvictAhead<THREADS>& ahead, const TwoTurns& first, EvictLds<THREADS>& lds) {
   const int64_t unit = static_cast<int64_t>(b * e.dm.L + l) * e.dm.Hkv + g;
   float* const acc = e.acc + unit * e.acc_pitch;
   Candidate best = grow_sums<THREADS>(e, scores, pitch, lse2, acc, 0, e.n + 1, ahead.sums, first, lds);

@@ -33,7 +33,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
   const Dims& dm = a.dm;
   const int lane = threadIdx.x % 64, col = lane % 32, grp = lane / 32;
   const int wu = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const Place place(a);
+  const Place<LOGITS != Logits::kEvict> place(a);
   const int b = place.b, l = place.l, g = place.g, row_group = place.row_group;
   const int nodes = a.ks.c, rows = dm.G * nodes;
   const int n_c = a.lens != nullptr ? min(max(a.lens[b], 0), a.ks.n_c) : a.ks.n_c;
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
     for (int i = 0; i < 16; ++i) o[r][i] = 0.f;
   float* scores = nullptr;
   if constexpr (LOGITS != Logits::kNone)
-    if (row < rows) scores = a.scores + (static_cast<int64_t>(blockIdx.z) * dm.Hq + h) * a.score_pitch;
+    if (row < rows) scores = a.scores + (static_cast<int64_t>(b * dm.L + l) * dm.Hq + h) * a.score_pitch;
 
   const int tiles = (n + 31) / 32, per = (tiles + a.splits - 1) / a.splits, end = min(tiles, (place.sp + 1) * per);
   int x = place.sp * per + wu;
@@ -183,8 +183,8 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
     float* const lse2 = reinterpret_cast<float*>(lds + Lds<D>::kJoin);
     join_waves<float, D, kWaves, kWaves>(a, o_s, rows_s, b, l, g, 0, here, place.sp, lse2);
     __syncthreads();
-    const float* const unit = a.scores + (static_cast<int64_t>(blockIdx.z) * dm.Hq + g * dm.G) * a.score_pitch;
-    evict_unit<64 * kWaves>(ev, b, l, g, unit, a.score_pitch, lse2, ahead, first_logits(ev, unit, a.score_pitch, 0, ev.n + 1),
+    const float* const unit = a.scores + (static_cast<int64_t>(b * dm.L + l) * dm.Hq + g * dm.G) * a.score_pitch;
+    evict_unit<64 * kWaves>(ev, b, l, g, unit, a.score_pitch, lse2, ahead, first_turns<64 * kWaves>(ev, unit, a.score_pitch, 0, ev.n + 1),
                             *reinterpret_cast<EvictLds<64 * kWaves>*>(lse2 + 32));
   } else {
     join_waves<float, D, kWaves, kWaves>(a, o_s, rows_s, b, l, g, row_group * 32, here, place.sp);

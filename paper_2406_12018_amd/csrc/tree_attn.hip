@@ -63,7 +63,11 @@ FewRowsPlan plan_for(int dtype, const Dims& dm, int nodes, int most_keys, bool l
 
 hipError_t launch_main(int dtype, FewRows& a, const FewRowsPlan& p, const EvictStep* ev, hipStream_t st) {
   a.splits = p.splits;
+  a.row_groups = p.row_groups;
+  a.units = static_cast<int>(workgroups(a.dm, p) / p.row_groups * p.splits);
   a.by_splits = fast_div(p.splits);
+  a.by_heads = fast_div(a.dm.Hkv);
+  a.by_eights = fast_div(8 * p.row_groups);
   a.by_layers = fast_div(a.dm.L);
   a.by_nodes = fast_div(a.ks.c);
   a.part_o = nullptr;
