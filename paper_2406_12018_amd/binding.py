@@ -339,27 +339,28 @@ def alloc_generation_workspace(cfg: Config, draft_len: int = 1, device="cuda") -
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _misfit(what: str, t, dtype, shape, device: int):
-    raise ValueError(f"{what}: {t.dtype} of shape {tuple(t.shape)} on device {t.get_device()}, expected {dtype} of "
-                     f"{tuple('any' if n is None else n for n in shape)} on device {device}")
+def _misfit(what: str, t, dtype, shape, device: int, more: str = ""):
+    raise ValueError(f"{what}: {t.dtype} of shape {tuple(t.shape)} on device {t.get_device()}, expected {dtype} of {shape}{more} on "
+                     f"device {device}")
 
 
 def _states(what: str, t, dtype, shape: tuple, device: int) -> CTensor:
     """citrus_tensor of t, which has to have this type and shape [B, L, heads, rows, d], on `device`."""
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
         _misfit(what, t, dtype, shape, device)
-    s = t.stride()
-    if s[4] != 1:
+    sb, sl, sh, ss, sd = t.stride()
+    if sd != 1:
         raise ValueError(f"{what}: expected a [B, L, H, S, d] tensor with contiguous last axis")
-    return CTensor(t.data_ptr(), s[0], s[1], s[2], s[3])
+    return CTensor(t.data_ptr(), sb, sl, sh, ss)
 
 
 def _cache(what: str, t, dtype, shape: tuple, device: int) -> CTensor:
     """The same of a cache, which may have more rows."""
     have = t.shape
-    if len(have) != 5 or have[3] < shape[3]:
-        _misfit(what, t, dtype, shape, device)
-    return _states(what, t, dtype, (*shape[:3], have[3], shape[4]), device)
+    if len(have) == 5 and have[3] >= shape[3]:
+        b, l, h, _, d = shape
+        return _states(what, t, dtype, (b, l, h, have[3], d), device)
+    _misfit(what, t, dtype, shape, device, " with that many rows or more")
 
 
 def _dense(what: str, t, dtype, shape: tuple, device: int) -> Optional[int]:
@@ -367,14 +368,15 @@ def _dense(what: str, t, dtype, shape: tuple, device: int) -> Optional[int]:
     if t is None:
         return None
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
-        _misfit(what + " (dense)", t, dtype, shape, device)
+        _misfit(what, t, dtype, shape, device, ", dense,")
     return t.data_ptr()
 
 
-def _on(device: int):
-    """The device that a call's tensors are on has to be the current one: its stream and its kernels are used."""
+def _stream_on(device: int, stream) -> int:
+    """The stream of a call: the given one, else the current one.  The device that the tensors are on has to be the current one."""
     if device < 0 or device != torch.cuda.current_device():
         raise ValueError(f"the tensors are on {'the host' if device < 0 else f'device {device}'}, not on the current device")
+    return _raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _generation_block(workspace, device: int):
@@ -391,7 +393,7 @@ def citrus_tree_attn(cfg: Config, q, k_draft, v_draft, ancestors, k_cache, v_cac
     [B, nodes], or [nodes] for one tree in all documents, bit u of a node's word for node u, its own among them (without it there is no
     such node).  cache_lens: int32 [B] lengths of the documents, up to cache_len.  Returns out."""
     nodes, device, dtype = q.shape[3], q.get_device(), cfg.torch_dtype
-    _on(device)
+    stream = _stream_on(device, stream)
     if out is None:
         out = torch.empty_like(q)
     B, L, hq, d = cfg.batch, cfg.layers, cfg.q_heads, cfg.head_dim
@@ -407,7 +409,7 @@ def citrus_tree_attn(cfg: Config, q, k_draft, v_draft, ancestors, k_cache, v_cac
         _cache("k_cache", k_cache, dtype, cache, device) if cached else tensor(None),
         _cache("v_cache", v_cache, dtype, cache, device) if cached else tensor(None), cache_len,
         _dense("cache_lens", cache_lens, torch.int32, (B,), device), _states("out", out, dtype, rows, device),
-        _dense("lse", lse, torch.float32, (B, L, hq, nodes), device), block, size, _stream(stream))
+        _dense("lse", lse, torch.float32, (B, L, hq, nodes), device), block, size, stream)
     _check(st, "citrus_tree_attn")
     return out
 
@@ -417,7 +419,7 @@ def citrus_tree_commit(cfg: Config, k_draft, v_draft, path, accepted, k_cache, v
     """Puts the draft states path[b, :accepted[b]] behind the cache of every document b, in place; path int32 [B, path_len],
     accepted and cache_lens int32 [B].  Returns new_lens [B], the documents' new lengths."""
     nodes, device, dtype = k_draft.shape[3], k_draft.get_device(), cfg.torch_dtype
-    _on(device)
+    stream = _stream_on(device, stream)
     B = cfg.batch
     if new_lens is None:
         new_lens = torch.empty(B, dtype=torch.int32, device=k_draft.device)
@@ -429,7 +431,7 @@ def citrus_tree_commit(cfg: Config, k_draft, v_draft, path, accepted, k_cache, v
         nodes, _dense("path", path, torch.int32, (B, path_len), device), path_len,
         _dense("accepted", accepted, torch.int32, (B,), device), _cache("k_cache", k_cache, dtype, cache, device),
         _cache("v_cache", v_cache, dtype, cache, device), cache_len, _dense("cache_lens", cache_lens, torch.int32, (B,), device),
-        _dense("new_lens", new_lens, torch.int32, (B,), device), _stream(stream))
+        _dense("new_lens", new_lens, torch.int32, (B,), device), stream)
     _check(st, "citrus_tree_commit")
     return new_lens
 
@@ -441,7 +443,7 @@ def citrus_decode_evict_step(cfg: Config, q, k_new, v_new, k_cache, v_cache, acc
     states, and the first cfg.start_size are kept).  tokens: states put into the cache so far.  Updates the caches and acc in place;
     evicted: int32 [B, L, sel_heads], the row whose state went, or -1.  Returns out."""
     device, dtype = q.get_device(), cfg.torch_dtype
-    _on(device)
+    stream = _stream_on(device, stream)
     if out is None:
         out = torch.empty_like(q)
     B, L, hkv, d = cfg.batch, cfg.layers, cfg.kv_heads, cfg.head_dim
@@ -453,7 +455,7 @@ def citrus_decode_evict_step(cfg: Config, q, k_new, v_new, k_cache, v_cache, acc
         _states("v_new", v_new, dtype, state, device), _cache("k_cache", k_cache, dtype, cache, device),
         _cache("v_cache", v_cache, dtype, cache, device), _dense("acc", acc, torch.float32, (B, L, hkv, cfg.cache_capacity), device),
         tokens, recent, _states("out", out, dtype, row, device),
-        _dense("evicted", evicted, torch.int32, (B, L, cfg.sel_heads), device), block, size, _stream(stream))
+        _dense("evicted", evicted, torch.int32, (B, L, cfg.sel_heads), device), block, size, stream)
     _check(st, "citrus_decode_evict_step")
     return out
 

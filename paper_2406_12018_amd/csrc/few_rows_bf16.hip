@@ -180,10 +180,8 @@ __host__ __device__ inline int strip_pitch(int n) { return (n + 1 + 31) / 32 * 3
 
 // Where a single token's logits go: to the workspace, for other kernels; or the unit is one workgroup's, which evicts by them.
 enum class Logits { kNone, kKept, kEvict, kEvictInLds };
-// Does one row group hold all rows of a KV head, so that nobody else reads its keys?
-template <int WAVES, int KH, Logits LOGITS>
-constexpr bool kAlone = !(WAVES == 8 && KH == 1) && LOGITS != Logits::kKept;
-template <int D, int WAVES, int KH, int PARTS, Logits LOGITS>
+// GROUPS: several row groups read the same keys.
+template <int D, int WAVES, int KH, int PARTS, Logits LOGITS, bool GROUPS>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictStep ev) {
   typedef Geo<D> T;
   constexpr bool kPrivate = KH == WAVES;
@@ -193,7 +191,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
   const Dims& dm = a.dm;
   const int lane = threadIdx.x % 64, col = lane % 32, grp = lane / 32;
   const int wu = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const Place<!kAlone<WAVES, KH, LOGITS>> at(a);
+  const Place<GROUPS> at(a);
   const int b = at.b, l = at.l, g = at.g, row_group = at.row_group;
   const int nodes = a.ks.c, rows = dm.G * nodes;
   const int n_c = a.lens != nullptr ? min(max(a.lens[b], 0), a.ks.n_c) : a.ks.n_c;
@@ -214,7 +212,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
   const int fill_row = lane / T::kSegs, fill_pos = lane % T::kSegs;
   // rows j0 + kR i + (0 .. kR - 1), kR rows from `first` on, to K rows at k_t and V rows at v_t.  Past the last state: the last.
   // What no other workgroup reads is loaded as not to be kept: 32 layers, budget 1024, 34.3 -> 30.6 us.
-  constexpr int kCachePolicy = kAlone<WAVES, KH, LOGITS> ? 2 : 0;  // nt
+  constexpr int kCachePolicy = GROUPS ? 0 : 2;  // nt
   auto fill = [&](int j0, int first, int count, char* k_t, char* v_t) {
     const bool in_cache = j0 + kR * (first + count) <= n_c;
 #pragma unroll
@@ -260,9 +258,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
     const int at_col = at_lane % 32, at_grp = at_lane / 32;
     const int at_row = min((row_group * kBlocks + wu / KH) * 32 + at_col, rows - 1);
     const int head = a.by_nodes.quotient(at_row), node = at_row - head * nodes;
-    uint64_t word = a.words != nullptr ? a.words[b * a.words_sb + node] : 1;
-    real = word >> node & 1;
-    if (nodes < 64) word &= (uint64_t{1} << nodes) - 1;
+    uint64_t word = 1;
     // per-lane LDS read offsets inside a tile, swizzle included
     uint32_t k_off[T::kKk], v_off[2 * T::kOut];
 #pragma unroll
@@ -274,6 +270,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
 
     bf16x8 q_op[T::kKk];
     auto load_queries = [&] {  // while the first keys are on their way; what is asked for later is counted from here
+      if (a.words != nullptr) word = a.words[b * a.words_sb + node];
       const uint16_t* qp = row_ptr<uint16_t>(a.q, b, l, g * dm.G + head, node) + 8 * at_grp;
 #pragma unroll
       for (int kk = 0; kk < T::kKk; ++kk) {
@@ -282,6 +279,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
         q_op[kk] = x.v;
       }
       wait_loads<0>();
+      real = word >> node & 1;
+      if (nodes < 64) word &= (uint64_t{1} << nodes) - 1;
     };
     c.m = -INFINITY;
     c.l = 0.f;
@@ -403,12 +402,12 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
   }
 }
 
-template <int D, int WAVES, int KH, int PARTS, Logits LOGITS>
+template <int D, int WAVES, int KH, int PARTS, Logits LOGITS, bool GROUPS = false>
 hipError_t launch(const FewRows& a, const EvictStep& ev, int row_groups, hipStream_t st) {
   typedef Lds<D, WAVES, KH> L;
   const int strip = LOGITS == Logits::kEvictInLds ? a.dm.G * strip_pitch(ev.n) * 4 : 0;
   static LdsLimit limit;
-  const auto kernel = few_rows_kernel<D, WAVES, KH, PARTS, LOGITS>;
+  const auto kernel = few_rows_kernel<D, WAVES, KH, PARTS, LOGITS, GROUPS>;
   const hipError_t e = raise_lds_limit(limit, reinterpret_cast<const void*>(kernel), LOGITS == Logits::kEvictInLds ? kLdsOfUnit - kLdsOfVote : L::kBytes);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(kernel, dim3(row_groups * a.splits, a.dm.Hkv, a.dm.B * a.dm.L), dim3(64 * WAVES), L::kBytes + strip, st, a, ev);
@@ -421,14 +420,17 @@ hipError_t launch_form(const FewRows& a, const FewRowsPlan& p, const EvictStep* 
     // the strip lies in LDS where that leaves as many workgroups to a compute unit as there are without it
     const int units = D == 128 ? 1 : 2;
     const bool fits = a.dm.G * strip_pitch(ev->n) * 4 + Lds<D, 4, 4>::kBytes <= kLdsOfUnit / units - kLdsOfVote;
-    return !p.evicts ? launch<D, 4, 4, 2, Logits::kKept>(a, none, p.row_groups, st)
-           : fits    ? launch<D, 4, 4, 2, Logits::kEvictInLds>(a, *ev, p.row_groups, st)
-                     : launch<D, 4, 4, 2, Logits::kEvict>(a, *ev, p.row_groups, st);
+    if (!p.evicts)
+      return p.row_groups > 1 ? launch<D, 4, 4, 2, Logits::kKept, true>(a, none, p.row_groups, st)
+                              : launch<D, 4, 4, 2, Logits::kKept>(a, none, 1, st);
+    return fits ? launch<D, 4, 4, 2, Logits::kEvictInLds>(a, *ev, 1, st) : launch<D, 4, 4, 2, Logits::kEvict>(a, *ev, 1, st);
   }
-  return p.kh == 4      ? launch<D, 4, 4, 2, Logits::kNone>(a, none, p.row_groups, st)
-         : p.waves == 4 ? launch<D, 4, 2, 2, Logits::kNone>(a, none, p.row_groups, st)
-         : p.kh == 2    ? launch<D, 8, 2, 2, Logits::kNone>(a, none, p.row_groups, st)
-                        : launch<D, 8, 1, D == 64 ? 2 : 1, Logits::kNone>(a, none, p.row_groups, st);
+  constexpr int kParts = D == 64 ? 2 : 1;  // from 129 rows on the matrix pipe counts
+  return p.kh == 4          ? launch<D, 4, 4, 2, Logits::kNone>(a, none, 1, st)
+         : p.waves == 4     ? launch<D, 4, 2, 2, Logits::kNone>(a, none, 1, st)
+         : p.kh == 2        ? launch<D, 8, 2, 2, Logits::kNone>(a, none, 1, st)
+         : p.row_groups > 1 ? launch<D, 8, 1, kParts, Logits::kNone, true>(a, none, p.row_groups, st)
+                            : launch<D, 8, 1, kParts, Logits::kNone>(a, none, 1, st);
 }
 
 }  // namespace

@@ -38,23 +38,26 @@ FewRowsPlan form_of(int dtype, const Dims& dm, int nodes, bool logits) {
 }
 int64_t workgroups(const Dims& dm, const FewRowsPlan& p) { return static_cast<int64_t>(dm.B) * dm.L * dm.Hkv * p.row_groups; }
 int most_splits(int dtype, const Dims& dm, const FewRowsPlan& p) {
-  const int64_t s = 4 * slots_of(dtype, dm) / workgroups(dm, p);
+  const int64_t s = 8 * slots_of(dtype, dm) / workgroups(dm, p);
   return static_cast<int>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
 }
 
-// Ranges of keys.  Rounds of the chip times a workgroup's share of the keys is what a launch takes; another launch to join the ranges
-// costs about as much as eight 32-key tiles of a workgroup's stream, an eviction's own launch fourteen, an eviction within the launch four.
+// Ranges of keys.  What a launch takes is counted in 32-key tiles of a workgroup's stream: the rounds of the chip times a workgroup's share of
+// the keys, six tiles for its start and end, and with several ranges the parts of its rows, written and read (a sixteenth of a tile
+// each).  An eviction within the launch is four more; another launch costs eight, one that evicts fourteen.
 FewRowsPlan plan_for(int dtype, const Dims& dm, int nodes, int most_keys, bool logits, bool may_evict) {
   FewRowsPlan p = form_of(dtype, dm, nodes, logits);
   const int64_t groups = workgroups(dm, p), slots = slots_of(dtype, dm);
   const int unit = p.kh == 4 ? 32 : 64, tiles = (most_keys + unit - 1) / unit;
+  const int rows = dm.G * nodes < 32 * p.waves / p.kh ? dm.G * nodes : 32 * p.waves / p.kh;
   int64_t best = INT64_MAX;
   for (int s = 1; s <= most_splits(dtype, dm, p); ++s) {
     const int per = (tiles + s - 1) / s;
     if (s > 1 && per * unit < 128) break;
     if ((tiles + per - 1) / per != s) continue;  // no empty ranges
-    const int behind = logits ? (s == 1 && may_evict ? 4 : 14) : s > 1 ? 8 : 0;
-    const int64_t cost = (s * groups + slots - 1) / slots * (per * unit / 32 + 6 + (s == 1 && may_evict ? 4 : 0)) + (behind == 4 ? 0 : behind);
+    const bool evicts = may_evict && s == 1;
+    const int64_t rounds = (s * groups + slots - 1) / slots, each = per * unit / 32 + 6 + (evicts ? 4 : 0) + (s > 1 ? rows / 16 : 0);
+    const int64_t cost = rounds * each + (evicts ? 0 : logits ? 14 : s > 1 ? 8 : 0);
     if (cost < best) best = cost, p.splits = s;
   }
   p.evicts = may_evict && p.splits == 1;

@@ -105,7 +105,7 @@ def test_the_binding_refuses_tensors_that_do_not_fit(monkeypatch):
                 k_cache=f(2, 1, 2, 80, 64), v_cache=f(2, 1, 2, 80, 64), cache_len=16)
     with pytest.raises(ValueError, match="host"):
         api.citrus_tree_attn(c, **good)
-    monkeypatch.setattr(B, "_on", lambda device: None)  # from here on the shapes are looked at
+    monkeypatch.setattr(B, "_stream_on", lambda device, stream: 0)  # from here on the shapes are looked at
     for name, bad in (("k_draft", f(2, 1, 2, 7, 64)), ("v_draft", f(2, 1, 4, 8, 64)), ("k_cache", f(2, 1, 2, 15, 64)),
                       ("v_cache", f(2, 1, 2, 80, 64, dtype=torch.bfloat16)), ("q", f(2, 1, 4, 8, 128)), ("ancestors", i32(2, 8)),
                       ("ancestors", torch.zeros((2, 7), dtype=torch.int64)), ("ancestors", torch.zeros((8, 2), dtype=torch.int64).t()),
