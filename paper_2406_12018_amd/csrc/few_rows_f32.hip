@@ -49,12 +49,20 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
   float4 q[kPieces], k[kPieces];
 #pragma unroll
   for (int i = 0; i < kPieces; ++i) q[i] = *reinterpret_cast<const float4*>(row_ptr<float>(a.q, b, l, h, t) + 8 * i + 4 * grp);
-  auto state = [&](const Segments& s, int j) {  // past the last state: the last
+  // Row j of the document's states.  (The views' fields are read here, once: chosen per lane, they were loaded again for every row, and a
+  // step over 88 layers of 854 states took 208 us.)
+  struct Rows {
+    const float *cache, *own;
+    int64_t ss_cache, ss_own;
+  };
+  const Rows ks{row_ptr<float>(a.ks.cache, b, l, g, 0), row_ptr<float>(a.ks.chunk, b, l, g, 0), a.ks.cache.ss, a.ks.chunk.ss};
+  const Rows vs{row_ptr<float>(a.vs.cache, b, l, g, 0), row_ptr<float>(a.vs.chunk, b, l, g, 0), a.vs.cache.ss, a.vs.chunk.ss};
+  auto state = [&](const Rows& r, int j) {  // past the last state: the last
     j = min(j, n - 1);
-    return j < n_c ? row_ptr<float>(s.cache, b, l, g, j) : row_ptr<float>(s.chunk, b, l, g, j - n_c);
+    return j < n_c ? r.cache + j * r.ss_cache : r.own + (j - n_c) * r.ss_own;
   };
   auto load_keys = [&](int x) {
-    const float* p = state(a.ks, 32 * x + col) + 4 * grp;
+    const float* p = state(ks, 32 * x + col) + 4 * grp;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) k[i] = *reinterpret_cast<const float4*>(p + 8 * i);
   };
@@ -70,14 +78,17 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
     if (row < rows) scores = a.scores + (static_cast<int64_t>(b * dm.L + l) * dm.Hq + h) * a.score_pitch;
 
   const int tiles = (n + 31) / 32, per = (tiles + a.splits - 1) / a.splits, end = min(tiles, (place.sp + 1) * per);
+  const float* const v_lane = vs.cache + 4 * grp * vs.ss_cache + kOut * col;
   int x = place.sp * per + wu;
+  const int whole = min(end, n_c / 32);  // tiles of cached states that every row sees
   if (x < end) load_keys(x);
-  for (; x < end; x += kWaves) {
+  auto turn = [&]<bool LAST>() {
     const int j0 = 32 * x, own = j0 - n_c;
     Values<D> v;  // of key 8 (i / 4) + 4 grp + i % 4: elements kOut col .. + kOut - 1
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float* p = state(a.vs, j0 + 8 * (i / 4) + 4 * grp + i % 4) + kOut * col;
+      const int key = 8 * (i / 4) + i % 4;
+      const float* p = LAST ? state(vs, j0 + key + 4 * grp) + kOut * col : v_lane + (j0 + key) * vs.ss_cache;
       if constexpr (kOut == 4) {
         const float4 w = *reinterpret_cast<const float4*>(p);
         v.x[i][0] = w.x, v.x[i][1] = w.y, v.x[i][2] = w.z, v.x[i][3] = w.w;
@@ -97,9 +108,8 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
       s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i].w, q[i].w, s, 0, 0, 0);
     }
     if (x + kWaves < end) load_keys(x + kWaves);
-    const bool last = own + 32 > 0;  // keys that not every row sees
-    const uint32_t seen = last ? seen_keys(word, own) : ~0u;
-    if (last) {
+    const uint32_t seen = LAST ? seen_keys(word, own) : ~0u;
+    if constexpr (LAST) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (!(seen >> (8 * (i / 4) + 4 * grp + i % 4) & 1)) s[i] = -INFINITY;
@@ -127,7 +137,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
     for (int r = 0; r < kOut; ++r)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[r][i] *= alpha;
-    if (last) {
+    if constexpr (LAST) {
       // 0 x infinity is NaN: values that are infinite or NaN are taken out, and their products added to the rows that see them
       float zero = 0.f;
 #pragma unroll
@@ -142,7 +152,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
 #pragma unroll
           for (int i = 0; i < 16; ++i) pk = at == i ? p[i] : pk;
           pk = __shfl(pk, col + 32 * (key / 4 % 2), 64);
-          const float* value = state(a.vs, j0 + key);
+          const float* value = state(vs, j0 + key);
           const bool sees = seen >> key & 1;
 #pragma unroll
           for (int r = 0; r < kOut; ++r)
@@ -162,7 +172,10 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_f32_kernel(FewRows a, Ev
     for (int i = 0; i < 16; ++i)
 #pragma unroll
       for (int r = 0; r < kOut; ++r) o[r] = __builtin_amdgcn_mfma_f32_32x32x2f32(v.x[i][r], p[i], o[r], 0, 0, 0);
-  }
+    x += kWaves;
+  };
+  while (x < whole) turn.template operator()<false>();
+  while (x < end) turn.template operator()<true>();
 
   sum += __shfl_xor(sum, 32, 64);
   float* const o_s = reinterpret_cast<float*>(lds);
