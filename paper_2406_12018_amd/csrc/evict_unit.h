@@ -78,6 +78,17 @@ __device__ inline Logits4 load_logits(const float* scores, int64_t pitch, int h,
   for (int x = 0; x < 4; ++x) l.s[x] = *reinterpret_cast<const float4*>(scores + min(h + x, G - 1) * pitch + j);
   return l;
 }
+// w += their weights.  lse2: by head, in LDS.
+__device__ inline void add_weights(const Logits4& l, const float* lse2, int h, int G, float (&w)[4]) {
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const float z = h + x < G ? lse2[h + x] : INFINITY;
+    w[0] += __builtin_amdgcn_exp2f(l.s[x].x - z);
+    w[1] += __builtin_amdgcn_exp2f(l.s[x].y - z);
+    w[2] += __builtin_amdgcn_exp2f(l.s[x].z - z);
+    w[3] += __builtin_amdgcn_exp2f(l.s[x].w - z);
+  }
+}
 // Sums of the keys [begin, end) of a unit grow, four keys and four heads a thread and turn, the logits two turns ahead; begin is a multiple
 // of 4.  scores: [head][pitch], lse2: by head.  old, first, second: load_sums of the thread's first keys, the logits of its first turns.
 // Returns this thread's smallest.
@@ -113,14 +124,7 @@ __device__ inline Candidate grow_sums(const EvictStep& e, const float* scores, i
 #pragma unroll
       for (int x = 0; x < 4; ++x) w[x] = 0.f;
     }
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const float z = t.h + x < G ? lse2[t.h + x] : INFINITY;
-      w[0] += __builtin_amdgcn_exp2f(l.s[x].x - z);
-      w[1] += __builtin_amdgcn_exp2f(l.s[x].y - z);
-      w[2] += __builtin_amdgcn_exp2f(l.s[x].z - z);
-      w[3] += __builtin_amdgcn_exp2f(l.s[x].w - z);
-    }
+    add_weights(l, lse2, t.h, G, w);
     if (t.h + 4 < G) continue;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
