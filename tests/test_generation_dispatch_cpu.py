@@ -1,0 +1,153 @@
+"""Generation over a retained cache without a GPU: which kernels a call launches, that every launch fits a grid, and what a failed launch
+leaves.  The calls run in a child process behind the stand-in for the HIP runtime; this file is the child's program too."""
+
+import ctypes as C
+import json
+import os
+import subprocess
+import sys
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+if __name__ == "__main__":
+    sys.path[:0] = [ROOT, os.path.join(ROOT, "tests")]
+
+from test_dispatch_cpu import Fake, Recorder  # noqa: E402
+
+
+# ---- in the child ----
+def fakes(api):
+    import torch
+
+    class Tensor(Fake):
+        dtype = torch.bfloat16
+
+        def get_device(self):
+            return 0
+
+        def is_contiguous(self):
+            return True
+
+    def make(kind, *shape, at=1 << 20):
+        t = Tensor(*shape, at=at)
+        t.dtype = kind
+        return t
+
+    api.binding._stream_on = lambda device, stream: 0
+    return make, torch
+
+
+def tree(api, launches, cases):
+    make, torch = fakes(api)
+    out = []
+    for B, L, Hq, Hkv, d, T, n, f32, fail in cases:
+        kind = torch.float32 if f32 else torch.bfloat16
+        cfg = api.Config(batch=B, layers=L, q_heads=Hq, kv_heads=Hkv, head_dim=d, chunk_len=1, budget=1, instr_len=1,
+                         dtype=api.F32 if f32 else api.BF16, cache_capacity=max(n, 1))
+        q, draft, cache = (make(kind, B, L, h, s, d, at=(i + 1) << 24) for i, (h, s) in enumerate(((Hq, T), (Hkv, T), (Hkv, max(n, 1)))))
+        ws = make(torch.uint8, api.generation_workspace_bytes(cfg, T), at=1 << 30)
+        ws.nbytes = ws.numel()
+        words, status = make(torch.int64, T), [0]
+
+        def call():
+            try:
+                api.citrus_tree_attn(cfg, q, draft, draft, words, cache, cache, n, out=make(kind, B, L, Hq, T, d, at=1 << 40), workspace=ws)
+            except api.CitrusError as e:
+                status[0] = e.status
+
+        got = [x for x in launches(call, fail) if x[0] != "lds"]
+        out.append([status[0], got])
+    return out
+
+
+def evict(api, launches, cases):
+    make, torch = fakes(api)
+    out = []
+    for B, L, Hq, Hkv, d, n, f32, per_layer, fail in cases:
+        kind = torch.float32 if f32 else torch.bfloat16
+        cfg = api.Config(batch=B, layers=L, q_heads=Hq, kv_heads=Hkv, head_dim=d, chunk_len=1, budget=n, instr_len=1,
+                         dtype=api.F32 if f32 else api.BF16, cache_capacity=n, select_mode=per_layer)
+        q, state, cache = (make(kind, B, L, h, s, d, at=(i + 1) << 24) for i, (h, s) in enumerate(((Hq, 1), (Hkv, 1), (Hkv, n))))
+        ws = make(torch.uint8, api.generation_workspace_bytes(cfg, 1), at=1 << 30)
+        ws.nbytes = ws.numel()
+        acc, status = make(torch.float32, B, L, Hkv, n), [0]
+
+        def call():
+            try:
+                api.citrus_decode_evict_step(cfg, q, state, state, cache, cache, acc, n + 3, 1, out=make(kind, B, L, Hq, 1, d, at=1 << 40), workspace=ws)
+            except api.CitrusError as e:
+                status[0] = e.status
+
+        got = [x for x in launches(call, fail) if x[0] != "lds"]
+        out.append([status[0], got])
+    return out
+
+
+# ---- in the test ----
+def in_child(body, tmp_path, **kw):
+    shim = str(tmp_path / "fake_hip.so")
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-o", shim, os.path.join(ROOT, "tests", "fake_hip.cpp")])
+    done = subprocess.run([sys.executable, os.path.abspath(__file__), shim, body.__name__, json.dumps(kw)], cwd=ROOT, stdout=subprocess.PIPE,
+                          stderr=subprocess.PIPE, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-3000:]
+    return json.loads(done.stdout.splitlines()[-1])
+
+
+def names(launches):
+    return [x[0].split("<")[0] for x in launches]
+
+
+def test_forms_of_the_attention(tmp_path):
+    """By rows of a KV head: private tiles up to 32, waves that share stages beyond, row groups from 257 on; ranges of keys where few units
+    have many; another launch only to join these."""
+    wants = {(1, 32, 32, 8, 128, 8, 900): ["few_rows_kernel<128, 4, 4"], (1, 32, 32, 8, 128, 9, 900): ["few_rows_kernel<128, 4, 2"],
+             (1, 32, 32, 8, 128, 17, 900): ["few_rows_kernel<128, 8, 2"], (1, 32, 32, 8, 128, 33, 900): ["few_rows_kernel<128, 8, 1"],
+             (1, 32, 64, 8, 128, 64, 900): ["few_rows_kernel<128, 8, 1"], (1, 1, 32, 8, 64, 1, 9000): ["few_rows_kernel<64, 4, 4", "join_ranges_kernel"],
+             (1, 1, 8, 8, 64, 1, 20): ["few_rows_kernel<64, 4, 4"]}
+    got = in_child(tree, tmp_path, cases=[[*c, False, -1] for c in wants])
+    for (case, want), (status, launches) in zip(wants.items(), got):
+        assert status == 0 and len(launches) == len(want), (case, launches)
+        for launch, name in zip(launches, want):
+            assert launch[0].startswith(name), (case, launches)
+    assert [x[1][0][1] for x in got[:5]] == [[1, 8, 32]] * 4 + [[2, 8, 32]]
+
+
+def test_largest_configurations_fit_a_grid(tmp_path):
+    """The most heads, the widest groups, and the longest caches that a configuration may have."""
+    cases = [[1, 65535, 64, 64, 64, 1, 5, f32, -1] for f32 in (False, True)]
+    cases += [[1, 8, 65535, 1, 64, 64, 70, f32, -1] for f32 in (False, True)] + [[1, 1, 65535, 65535, 128, 64, 3, f32, -1] for f32 in (False, True)]
+    cases += [[1, 1, 8, 1, 128, 64, (1 << 31) // 512 - 1, f32, -1] for f32 in (False, True)]
+    for case, (status, launches) in zip(cases, in_child(tree, tmp_path, cases=cases)):
+        assert status == 0 and launches, (case, status)
+    cases = [[1, 65535, 64, 64, 64, 5, f32, p, -1] for f32 in (False, True) for p in (0, 1)] + [[1, 1, 1024, 1, 64, 70, f32, 0, -1] for f32 in (False, True)]
+    cases += [[1, 1, 8, 1, 128, (1 << 31) // 512 - 1, f32, p, -1] for f32 in (False, True) for p in (0, 1)]
+    for case, (status, launches) in zip(cases, in_child(evict, tmp_path, cases=cases)):
+        assert status == 0 and launches, (case, status)
+
+
+def test_forms_of_the_eviction(tmp_path):
+    """Within the launch that attends where the units fill the chip once; behind it a workgroup per unit, or per layer of few heads; ranges
+    of keys for long caches and for layers of many heads."""
+    wants = {(1, 32, 32, 8, 128, 1024, False, 0): ["few_rows_kernel"], (1, 1, 32, 8, 128, 2000, False, 0): ["few_rows_kernel", "evict_unit_kernel"],
+             (1, 1, 33, 1, 128, 700, False, 0): ["few_rows_kernel", "evict_unit_kernel"],
+             (1, 1, 8, 8, 128, 9000, False, 0): ["few_rows_kernel", "grow_sums_kernel", "make_room_kernel"],
+             (1, 4, 16, 4, 128, 2000, False, 1): ["few_rows_kernel", "evict_layer_kernel"],
+             (1, 4, 32, 8, 128, 2000, False, 1): ["few_rows_kernel", "grow_sums_kernel", "make_room_kernel"],
+             (2, 128, 8, 2, 64, 200, True, 0): ["few_rows_f32_kernel"], (1, 4, 16, 4, 64, 500, True, 1): ["few_rows_f32_kernel", "evict_layer_kernel"]}
+    got = in_child(evict, tmp_path, cases=[[*c, -1] for c in wants])
+    for (case, want), (status, launches) in zip(wants.items(), got):
+        assert status == 0 and names(launches) == want, (case, launches)
+
+
+def test_failed_launches_are_reported(tmp_path):
+    from paper_2406_12018_amd import binding as B
+    got = in_child(tree, tmp_path, cases=[[1, 1, 32, 8, 128, 8, 4000, False, at] for at in (0, 1, 2)])
+    assert [(x[0], len(x[1])) for x in got] == [(B.ERR_DEVICE, 0), (B.ERR_DEVICE, 1), (0, 2)]
+    got = in_child(evict, tmp_path, cases=[[1, 1, 8, 8, 128, 9000, False, 0, at] for at in (0, 1, 2, 3)])
+    assert [(x[0], len(x[1])) for x in got] == [(B.ERR_DEVICE, 0), (B.ERR_DEVICE, 1), (B.ERR_DEVICE, 2), (0, 3)]
+
+
+if __name__ == "__main__":
+    fake = C.CDLL(sys.argv[1], C.RTLD_GLOBAL)  # before anything that loads the real runtime
+    import paper_2406_12018_amd as api_
+
+    print(json.dumps(globals()[sys.argv[2]](api_, Recorder(fake, api_.binding._lib()), **json.loads(sys.argv[3]))))

@@ -112,6 +112,16 @@ LARGE = {
     "layers_of_two_waves": dict(B=1, L=33, Hq=32, Hkv=8, d=128, budget=1025, recent=100),
     "group_of_8": dict(B=2, L=40, Hq=64, Hkv=8, d=128, budget=2047, recent=300),
     "group_of_33": dict(B=1, L=2, Hq=33, Hkv=1, d=64, budget=700, recent=3),
+    "one_round": dict(B=1, L=32, Hq=32, Hkv=8, d=128, budget=1024, recent=128, start=4),          # within the launch, logits in LDS
+    "one_round_global": dict(B=1, L=32, Hq=64, Hkv=8, d=128, budget=2000, recent=100, start=1),   # ... in the workspace
+    "one_round_64": dict(B=2, L=32, Hq=32, Hkv=8, d=64, budget=900, recent=64),
+    "one_round_64_global": dict(B=2, L=32, Hq=40, Hkv=8, d=64, budget=1500, recent=7),
+    "unit_kernel_at_its_end": dict(B=1, L=1, Hq=5, Hkv=1, d=64, budget=8191, recent=10),
+    "ranges_from_here": dict(B=1, L=1, Hq=5, Hkv=1, d=64, budget=8192, recent=10, start=4),
+    "layer_kernel_at_its_end": dict(B=1, L=2, Hq=16, Hkv=4, d=64, budget=2047, recent=90, per_layer=True),
+    "layer_ranges_from_here": dict(B=1, L=2, Hq=16, Hkv=4, d=64, budget=2048, recent=90, per_layer=True, start=4),
+    "layer_of_many_heads": dict(B=2, L=2, Hq=24, Hkv=6, d=128, budget=333, recent=20, per_layer=True),
+    "layer_of_one_wide_group": dict(B=1, L=1, Hq=37, Hkv=1, d=64, budget=130, recent=20, per_layer=True),
     "chip_full_wide_group": dict(B=1, L=260, Hq=16, Hkv=1, d=64, budget=1600, recent=3),
 }
 

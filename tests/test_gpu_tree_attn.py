@@ -56,6 +56,7 @@ SHAPES = [  # B, L, Hq, Hkv, d, T, n
     (1, 1, 2, 2, 128, 33, 129), (1, 1, 8, 2, 128, 16, 255), (1, 1, 8, 2, 64, 17, 500), (1, 1, 8, 1, 128, 33, 300), (1, 1, 16, 2, 128, 64, 97),
     (1, 1, 40, 1, 128, 3, 200), (1, 1, 40, 1, 64, 64, 70), (3, 1, 2, 1, 64, 63, 0), (1, 3, 3, 3, 128, 64, 1), (1, 1, 8, 8, 128, 7, 1300),
     (1, 1, 4, 1, 128, 1, 4500), (1, 1, 8, 2, 64, 13, 5000), (1, 1, 8, 1, 128, 40, 2500), (2, 70, 4, 2, 64, 4, 40),
+    (2, 5, 16, 1, 128, 64, 90), (1, 11, 9, 1, 64, 60, 33), (1, 1, 4, 1, 128, 64, 3000), (3, 3, 4, 1, 128, 40, 260),
 ]
 
 
@@ -118,6 +119,14 @@ def _with(case, kd, vd):
         return case.run()
     finally:
         case.kd, case.vd = kept
+
+
+def test_bits_behind_the_draft_are_ignored():
+    case = Case(4, 1, 1, 8, 2, 128, 9, 50)
+    want = case.run()
+    case.words = [[w | 0xABCD << 40 | 1 << 63 | 1 << 9 for w in doc] for doc in case.words]
+    for a, b in zip(case.run(), want):
+        same_bits(a, b)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
