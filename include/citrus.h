@@ -332,7 +332,8 @@ int32_t citrus_decode_step(const citrus_config* cfg, citrus_tensor q, citrus_ten
  * for documents of different lengths.
  *
  * q, out             [B, L, Hq, draft_len, d]; 1 <= draft_len <= 64; out must not overlap an input
- * k_draft, v_draft   [B, L, Hkv, draft_len, d]: the nodes' own states (nothing is appended to the cache)
+ * k_draft, v_draft   [B, L, Hkv, draft_len, d]: the nodes' own states (nothing is appended to the cache; they may lie in the caches'
+ *                    memory, behind the cache_len rows)
  * ancestors          device, 8-byte aligned; ancestors_stride_b words from one document to the next: >= draft_len, or 0
  *                    where all documents share one tree
  * k_cache, v_cache   [B, L, Hkv, >= cache_len, d]   (ptr may be NULL iff cache_len == 0)
@@ -383,7 +384,8 @@ int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citr
  * depend on the order of its states.)  With start_size + recent == budget this is a sliding window behind the first states.
  * cfg->select_mode PER_LAYER: one row for all KV heads of a layer, by the sum of their sums in head order.
  *
- * q, out         [B, L, Hq, 1, d];  k_new, v_new  [B, L, Hkv, 1, d]: the token's own state; out must not overlap an input
+ * q, out         [B, L, Hq, 1, d];  k_new, v_new  [B, L, Hkv, 1, d]: the token's own state, not in the caches' memory; out must not
+ *                overlap an input
  * k_cache, v_cache [B, L, Hkv, >= min(tokens + 1, budget), d], in/out
  * acc            dense f32 [B, L, Hkv, cache_capacity], in/out: the states' sums
  * tokens         states that have been put into this cache so far, evicted ones included; the caller's count becomes tokens + 1.  A

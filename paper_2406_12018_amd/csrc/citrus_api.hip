@@ -413,12 +413,13 @@ citrus_status check_generation_workspace(const citrus_config* c, int draft_len, 
 template <typename T>
 bool misaligned(const T* p) { return reinterpret_cast<uintptr_t>(p) % sizeof(T) != 0; }
 citrus_status check_draft(const citrus_config* c, int draft_len, int cache_len, const citrus_tensor& k_draft, const citrus_tensor& v_draft,
-                          const citrus_tensor& k_cache, const citrus_tensor& v_cache, const int32_t* cache_lens) {
+                          const citrus_tensor& k_cache, const citrus_tensor& v_cache, const int32_t* cache_lens, bool written) {
   if (draft_len < 1 || draft_len > kMaxNodes) return CITRUS_ERR_SHAPE;
   if (cache_len < 0 || cache_len > c->cache_capacity || misaligned(cache_lens)) return CITRUS_ERR_SHAPE;
   CITRUS_TRY(check_tensor(c, k_draft, draft_len, false));
   CITRUS_TRY(check_tensor(c, v_draft, draft_len, false));
-  if (k_draft.ptr == k_cache.ptr || v_draft.ptr == v_cache.ptr) return CITRUS_ERR_SHAPE;
+  // (an empty cache may begin with the draft)
+  if ((written || cache_len > 0) && (k_draft.ptr == k_cache.ptr || v_draft.ptr == v_cache.ptr)) return CITRUS_ERR_SHAPE;
   return CITRUS_OK;
 }
 
@@ -592,7 +593,7 @@ int32_t citrus_tree_attn(const citrus_config* cfg, citrus_tensor q, citrus_tenso
                          int32_t cache_len, const int32_t* cache_lens, citrus_tensor out, float* lse, void* workspace,
                          size_t workspace_bytes, void* hip_stream) {
   CITRUS_TRY(check_config(cfg));
-  CITRUS_TRY(check_draft(cfg, draft_len, cache_len, k_draft, v_draft, k_cache, v_cache, cache_lens));
+  CITRUS_TRY(check_draft(cfg, draft_len, cache_len, k_draft, v_draft, k_cache, v_cache, cache_lens, false));
   if (ancestors == nullptr) return CITRUS_ERR_NULL;
   if (misaligned(ancestors) || misaligned(lse) || (ancestors_stride_b != 0 && ancestors_stride_b < draft_len)) return CITRUS_ERR_SHAPE;
   CITRUS_TRY(check_tensor(cfg, q, draft_len, false));
@@ -619,7 +620,7 @@ int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citr
                            const int32_t* path, int32_t path_len, const int32_t* accepted, citrus_tensor k_cache,
                            citrus_tensor v_cache, int32_t cache_len, const int32_t* cache_lens, int32_t* new_lens, void* hip_stream) {
   CITRUS_TRY(check_config(cfg));
-  CITRUS_TRY(check_draft(cfg, draft_len, cache_len, k_draft, v_draft, k_cache, v_cache, cache_lens));
+  CITRUS_TRY(check_draft(cfg, draft_len, cache_len, k_draft, v_draft, k_cache, v_cache, cache_lens, true));
   if (path == nullptr || accepted == nullptr) return CITRUS_ERR_NULL;
   if (path_len < 1 || path_len > kMaxNodes || misaligned(path) || misaligned(accepted) || misaligned(new_lens)) return CITRUS_ERR_SHAPE;
   CITRUS_TRY(check_tensor(cfg, k_cache, cfg->cache_capacity, false));

@@ -58,7 +58,7 @@ def test_tree_attention_refuses(status, kw):
     (B.ERR_SHAPE, dict(nodes=0)), (B.ERR_SHAPE, dict(nodes=65)), (B.ERR_SHAPE, dict(n=65)), (B.ERR_SHAPE, dict(path_len=0)),
     (B.ERR_SHAPE, dict(path_len=65)), (B.ERR_NULL, dict(path=None)), (B.ERR_NULL, dict(accepted=None)), (B.ERR_SHAPE, dict(path=0x8002)),
     (B.ERR_SHAPE, dict(accepted=0x8102)), (B.ERR_SHAPE, dict(new=0x8201)), (B.ERR_NULL, dict(kc=NULL)), (B.ERR_NULL, dict(vd=NULL)),
-    (B.ERR_SHAPE, dict(kd=at(0x5000))), (B.ERR_SHAPE, dict(new=0x7000, lens=0x7000)), (B.ERR_SHAPE, dict(new=0x8100)), (B.ERR_SHAPE, dict(new=0x8000)),
+    (B.ERR_SHAPE, dict(kd=at(0x5000))), (B.ERR_SHAPE, dict(kd=at(0x5000), n=0)), (B.ERR_SHAPE, dict(new=0x7000, lens=0x7000)), (B.ERR_SHAPE, dict(new=0x8100)), (B.ERR_SHAPE, dict(new=0x8000)),
 ])
 def test_commit_refuses(status, kw):
     assert commit(**kw) == status

@@ -92,6 +92,19 @@ def test_ragged_documents_and_padding(T, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [0, 1, 45, 300])
+def test_a_draft_in_the_memory_of_the_cache(n, dtype):
+    """Behind the cache's rows, or at its beginning where there are none."""
+    case = Case(9, 2, 2, 6, 2, 128, 7, n, dtype, cap=n + 9)
+    apart = case.run()
+    case.check(*apart)
+    case.kc[:, :, :, n:n + 7], case.vc[:, :, :, n:n + 7] = case.kd, case.vd
+    case.kd, case.vd = case.kc[:, :, :, n:n + 7], case.vc[:, :, :, n:n + 7]
+    for a, b in zip(case.run(), apart):
+        same_bits(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("Hq,n", [(2, 0), (2, 45), (10, 200), (10, 3000)])
 def test_what_a_node_does_not_see_does_not_touch_it(Hq, n, d, dtype):
