@@ -4,7 +4,8 @@
 // Every byte of K and V is read once, softmax on the way: running maximum and sum per row, accumulators in registers.  With R rows
 // of a head group a byte of K/V meets R flop: up to 128 rows the launch is the stream of K/V bytes, from about 256 on it is the
 // matrix pipe's and the vector units'.  Forms of one kernel, by rows:
-//   private  up to 32: every wave streams 32-key tiles of its own through LDS, with no barrier between the waves;
+//   private  up to 32: every wave streams 32-key tiles of its own through LDS, with no barrier between the waves; a unit to four waves,
+//            or to one wave where many units have few keys each;
 //   shared   more: the waves of a workgroup read the same 64-key stages, four of them in LDS, a block of 32 rows per KH waves (KH = 2, up
 //            to 128 rows: each takes half of a stage's keys; KH = 1, eight blocks to a workgroup), one barrier a stage.
 // Keys are split over workgroups where the units do not fill the chip; another launch joins the ranges.
@@ -187,7 +188,7 @@ enum class Logits { kNone, kKept, kEvict, kEvictInLds };
 //
 // GROUPS: several row groups read the same keys.  grid: (row groups * key ranges, Hkv, B * L)
 template <int D, int WAVES, int KH, int PARTS, Logits LOGITS, bool GROUPS>
-__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictStep ev) {
+__global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 2 : 1) void few_rows_kernel(FewRows a, EvictStep ev) {
   typedef Geo<D> T;
   constexpr bool kPrivate = KH == WAVES;
   constexpr int kBlocks = WAVES / KH;  // of 32 rows
@@ -370,7 +371,13 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows a, EvictSt
   for (int r = 0; r < T::kOut; ++r)
 #pragma unroll
     for (int i = 0; i < 16; ++i) zero = fmaf(c.o[r][i], 0.f, zero);
-  if (!__syncthreads_and(zero == 0.f || row >= rows || !real)) over_the_keys.template operator()<true>();
+  const bool good = zero == 0.f || row >= rows || !real;
+  bool all_good;
+  if constexpr (WAVES == 1)
+    all_good = __all(good);
+  else
+    all_good = __syncthreads_and(good);
+  if (!all_good) over_the_keys.template operator()<true>();
 
   // ---- the waves of a block of rows join through LDS (the tiles have been read when every wave is here) ----
   constexpr int kPitch = D + 4;
@@ -421,6 +428,10 @@ hipError_t launch(const FewRows& a, const EvictStep& ev, int row_groups, hipStre
 template <int D>
 hipError_t launch_form(const FewRows& a, const FewRowsPlan& p, const EvictStep* ev, hipStream_t st) {
   const EvictStep none{};
+  if (p.waves == 1)  // a unit to a wave; its logits, if any, in the workspace: a strip of them in LDS costs waves
+    return ev == nullptr ? launch<D, 1, 1, 2, Logits::kNone>(a, none, 1, st)
+           : p.evicts    ? launch<D, 1, 1, 2, Logits::kEvict>(a, *ev, 1, st)
+                         : launch<D, 1, 1, 2, Logits::kKept>(a, none, 1, st);
   if (ev != nullptr) {
     // the strip lies in LDS where that leaves as many workgroups to a compute unit as there are without it
     const int units = D == 128 ? 1 : 2;

@@ -42,9 +42,16 @@ int most_splits(int dtype, const Dims& dm, const FewRowsPlan& p) {
   return static_cast<int>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
 }
 
-// Ranges of keys.  What a launch takes is counted in 32-key tiles of a workgroup's stream: the rounds of the chip times a workgroup's share of
-// the keys, six tiles for its start and end, and with several ranges the parts of its rows, written and read (a sixteenth of a tile
-// each).  An eviction within the launch is four more; another launch costs eight, one that evicts fourteen.
+// Ranges of keys, and waves to a unit.  What a launch takes is counted in 32-key tiles of a workgroup's stream (0.6 us): the rounds of the
+// chip times a workgroup's share of the keys, six tiles for its start and end, and with several ranges the parts of its rows, written
+// and read (a sixteenth of a tile each).  An eviction within the launch is six more; another launch costs eight, one that evicts
+// fourteen.
+// Of units with few keys the start and the end are the most part.  A unit to a single wave (bf16, up to 32 rows) puts as many units on a
+// compute unit as their tiles fit its LDS, five at head_dim 128, and their starts and ends overlap.  They share its stream, of which one
+// alone reaches half; the last of them leave it idle in part; and a wave alone evicts more slowly the longer the unit is.  2560 units of
+// one row, head_dim 128, four waves and one: 30 states 46.9 and 18.4 us, 130 states 77.5 and 43.4, 300 states 94.7 and 80.5, 1000 states
+// 208 and 209, 4000 states 750 and 802; with two heads each and the eviction 81.8 and 30.9, 109 and 57.0, 136 and 94.9, 264 and 265, 962
+// and 1040.
 FewRowsPlan plan_for(int dtype, const Dims& dm, int nodes, int most_keys, bool logits, bool may_evict) {
   FewRowsPlan p = form_of(dtype, dm, nodes, logits);
   const int64_t groups = workgroups(dm, p), slots = slots_of(dtype, dm);
@@ -56,9 +63,15 @@ FewRowsPlan plan_for(int dtype, const Dims& dm, int nodes, int most_keys, bool l
     if (s > 1 && per * unit < 128) break;
     if ((tiles + per - 1) / per != s) continue;  // no empty ranges
     const bool evicts = may_evict && s == 1;
-    const int64_t rounds = (s * groups + slots - 1) / slots, each = per * unit / 32 + 6 + (evicts ? 4 : 0) + (s > 1 ? rows / 16 : 0);
+    const int64_t rounds = (s * groups + slots - 1) / slots, each = per * unit / 32 + 6 + (evicts ? 6 : 0) + (s > 1 ? rows / 16 : 0);
     const int64_t cost = rounds * each + (evicts ? 0 : logits ? 14 : s > 1 ? 8 : 0);
     if (cost < best) best = cost, p.splits = s;
+  }
+  if (dtype == CITRUS_BF16 && p.kh == 4 && p.row_groups == 1) {
+    const int64_t at_once = 256 * (dm.D == 128 ? 5 : may_evict ? 8 : 10), rounds = (groups + at_once - 1) / at_once;
+    const int64_t shares = (groups + slots - 1) / slots, idle = shares < 2 ? 0 : (shares < 5 ? shares : 5) - 2;
+    const int64_t streams = (shares < 2 * rounds ? 2 * rounds : shares) * tiles + idle * tiles / 2;
+    if (streams + rounds * (6 + (may_evict ? 6 + tiles : 0)) + (logits && !may_evict ? 14 : 0) < best) p.waves = p.kh = 1, p.splits = 1;
   }
   p.evicts = may_evict && p.splits == 1;
   return p;

@@ -111,6 +111,21 @@ def test_forms_of_the_attention(tmp_path):
     assert [x[1][0][1] for x in got[:5]] == [[1, 8, 32]] * 4 + [[2, 8, 32]]
 
 
+def test_a_unit_to_a_wave_where_many_have_few_keys(tmp_path):
+    wants = {(1, 64, 32, 8, 128, 1, 130): "128, 1, 1", (1, 32, 32, 8, 128, 1, 130): "128, 4, 4", (1, 160, 32, 8, 128, 1, 900): "128, 4, 4",
+             (1, 96, 32, 8, 64, 4, 130): "64, 1, 1", (1, 64, 32, 8, 64, 4, 130): "64, 4, 4", (1, 160, 32, 8, 64, 4, 1200): "64, 4, 4"}
+    got = in_child(tree, tmp_path, cases=[[*c, False, -1] for c in wants])
+    for (case, want), (status, launches) in zip(wants.items(), got):
+        assert status == 0 and len(launches) == 1 and launches[0][0].startswith(f"few_rows_kernel<{want},"), (case, launches)
+    wants = {(1, 160, 16, 8, 128, 130, False, 0): ["128, 1, 1"], (1, 32, 16, 8, 128, 130, False, 0): ["128, 4, 4"],
+             (1, 160, 16, 8, 128, 1000, False, 0): ["128, 4, 4"], (1, 160, 16, 8, 64, 130, False, 0): ["64, 1, 1"],
+             (1, 160, 16, 8, 128, 130, False, 1): ["128, 1, 1", "evict_layer_kernel"]}
+    got = in_child(evict, tmp_path, cases=[[*c, -1] for c in wants])
+    for (case, want), (status, launches) in zip(wants.items(), got):
+        assert status == 0 and len(launches) == len(want) and launches[0][0].startswith(f"few_rows_kernel<{want[0]},"), (case, launches)
+        assert names(launches)[1:] == want[1:]
+
+
 def test_largest_configurations_fit_a_grid(tmp_path):
     """The most heads, the widest groups, and the longest caches that a configuration may have."""
     cases = [[1, 65535, 64, 64, 64, 1, 5, f32, -1] for f32 in (False, True)]

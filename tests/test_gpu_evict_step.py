@@ -135,6 +135,28 @@ def test_full_caches_of_real_sizes(name, dtype):
         run.step()
 
 
+MANY_SHORT = {  # units that fill the chip more than once, with few states each
+    "one_state": dict(B=2, L=70, Hq=4, Hkv=2, d=128, budget=1, recent=1),
+    "tile_end": dict(B=1, L=140, Hq=4, Hkv=2, d=128, budget=63, recent=9, start=1),
+    "group_of_8": dict(B=2, L=66, Hq=16, Hkv=2, d=128, budget=130, recent=20, start=4),
+    "group_of_32": dict(B=1, L=300, Hq=32, Hkv=1, d=128, budget=65, recent=64),
+    "several_rounds": dict(B=2, L=700, Hq=2, Hkv=1, d=128, budget=257, recent=30, start=4),
+    "head_dim_64": dict(B=3, L=100, Hq=6, Hkv=2, d=64, budget=300, recent=77),
+    "head_dim_64_rounds": dict(B=1, L=2100, Hq=3, Hkv=1, d=64, budget=40, recent=5, cap=50),
+    "per_layer": dict(B=1, L=300, Hq=6, Hkv=2, d=128, budget=90, recent=10, start=2, per_layer=True),
+    "per_layer_64": dict(B=2, L=40, Hq=32, Hkv=8, d=64, budget=30, recent=10, per_layer=True),
+}
+
+
+@pytest.mark.parametrize("name", list(MANY_SHORT))
+def test_many_units_of_few_states(name):
+    run = Run(60, **MANY_SHORT[name])
+    for tokens in (0, run.cfg.budget - 1, run.cfg.budget, run.cfg.budget + 17):
+        run.tokens = tokens
+        run.step()
+        run.step()
+
+
 def test_equal_sums_the_lowest_row_goes():
     """Zero queries: every weight is the same number; sums of 1: the first row behind the start, then the next, as each eviction moves
     the oldest recent state, with a larger sum, into it."""

@@ -91,6 +91,46 @@ def test_ragged_documents_and_padding(T, d, dtype):
         same_bits(a, b)
 
 
+MANY_SHORT = [  # units that fill the chip more than once, with few keys each
+    (2, 65, 4, 2, 128, 1, 0), (2, 70, 8, 2, 128, 5, 37), (3, 50, 4, 2, 128, 16, 300), (1, 1400, 1, 1, 128, 3, 20), (1, 90, 6, 6, 64, 2, 130),
+    (2, 140, 8, 2, 64, 8, 31), (1, 2700, 1, 1, 64, 1, 33), (1, 32, 32, 32, 128, 1, 63),
+]
+
+
+@pytest.mark.parametrize("shape", MANY_SHORT, ids=lambda s: "x".join(map(str, s)))
+def test_many_units_of_few_keys(shape):
+    case = Case(12, *shape)
+    out, lse = case.run()
+    case.check(out, lse)
+    again, lse2 = case.run()
+    same_bits(out, again)
+    same_bits(lse, lse2)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_units_of_few_keys_ragged(d):
+    """Documents of other lengths, padding, and a branch whose states are NaN or infinite beside one that does not see them."""
+    lens, T = [0, 70, 31, 1, 64, 300], 6
+    case = Case(6, len(lens), 50, 6, 2, d, T, 70, lens=lens, trees=[6, 1, 2, 6, 3, 5], cap=75)
+    clean = case.run()
+    case.check(*clean)
+    for b, n in enumerate(case.lens):
+        case.kc[b, :, :, n:] = float("nan")
+        case.vc[b, :, :, n:] = float("-inf")
+    for a, b in zip(case.run(), clean):
+        same_bits(a, b)
+    case.words = [[sum(1 << u for u in range(t + 1) if u % 2 == t % 2) for t in range(T)]] * len(lens)
+    left, clean = [0, 2, 4], case.run()
+    case.check(*clean)
+    for bad_k, bad_v in ((float("nan"), 1.0), (1.0, float("inf"))):
+        kd, vd = case.kd.clone(), case.vd.clone()
+        kd[:, :, :, 1::2], vd[:, :, :, 1::2] = bad_k, bad_v
+        out, lse = _with(case, kd, vd)
+        same_bits(out[:, :, :, left], clean[0][:, :, :, left])
+        same_bits(lse[:, :, :, left], clean[1][:, :, :, left])
+        assert not torch.isfinite(out[:, :, :, 1::2].float()).any()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n", [0, 1, 45, 300])
 def test_a_draft_in_the_memory_of_the_cache(n, dtype):
