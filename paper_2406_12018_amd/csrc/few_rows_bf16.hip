@@ -24,7 +24,9 @@ namespace {
 typedef __attribute__((address_space(3))) void* lds_void_ptr;
 typedef __attribute__((address_space(3))) char* lds_char_ptr;
 
-constexpr int kStageKeys = 64, kStages = 4;  // shared form
+constexpr int kStageKeys = 64;  // shared form
+template <int D, int WAVES, int KH>
+constexpr int kStagesOf = D == 64 && WAVES == 4 && KH == 1 ? 3 : 4;  // three workgroups to a compute unit
 constexpr int kLdsOfUnit = 160 * 1024, kLdsOfVote = 1024;  // __syncthreads_and has some of its own, in front of the tiles
 
 // What the lanes of one query row hold of it.
@@ -174,7 +176,7 @@ template <int D, int WAVES, int KH>
 struct Lds {
   static constexpr int kRows = WAVES * 32 * (D + 4) * 4, kJoin = kRows + WAVES * 32 * 16;  // o_s, rows_s
   static constexpr int kAfter = kJoin + 32 * 4 + sizeof(EvictLds<64 * WAVES>);            // lse2
-  static constexpr int kTiles = KH == WAVES ? WAVES * Geo<D>::kWaveLdsBytes : kStages * (kStageKeys / 32) * 2 * Geo<D>::kTileBytes;
+  static constexpr int kTiles = KH == WAVES ? WAVES * Geo<D>::kWaveLdsBytes : kStagesOf<D, WAVES, KH> * (kStageKeys / 32) * 2 * Geo<D>::kTileBytes;
   static constexpr int kBytes = ((kAfter > kTiles ? kAfter : kTiles) + 15) / 16 * 16;  // ... the strip of logits
 };
 // A unit's logits in LDS: the pitch of a head.  Heads four words apart from the same bank.
@@ -192,6 +194,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 2 : 1) void few_rows_kerne
   typedef Geo<D> T;
   constexpr bool kPrivate = KH == WAVES;
   constexpr int kBlocks = WAVES / KH;  // of 32 rows
+  constexpr int kStages = kStagesOf<D, WAVES, KH>;
   constexpr int kTileBytes = T::kTileBytes, kR = T::kRowsPerLoad;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const Dims& dm = a.dm;
@@ -441,14 +444,13 @@ hipError_t launch_form(const FewRows& a, const FewRowsPlan& p, const EvictStep* 
                               : launch<D, 4, 4, 2, Logits::kKept>(a, none, 1, st);
     return fits ? launch<D, 4, 4, 2, Logits::kEvictInLds>(a, *ev, 1, st) : launch<D, 4, 4, 2, Logits::kEvict>(a, *ev, 1, st);
   }
+  if (p.kh == 4) return launch<D, 4, 4, 2, Logits::kNone>(a, none, 1, st);
+  if (p.kh == 2) return p.waves == 4 ? launch<D, 4, 2, 2, Logits::kNone>(a, none, 1, st) : launch<D, 8, 2, 2, Logits::kNone>(a, none, 1, st);
   // Two bf16 parts of a weight in P.V cost nothing where the stream of keys bounds; from 129 rows on, at head_dim 128, one: the error of
   // a row is then sqrt(2) times that of the rounding of its result (0.0023 against 0.0017 relative).
-  constexpr int kParts = D == 64 ? 2 : 1;
-  return p.kh == 4          ? launch<D, 4, 4, 2, Logits::kNone>(a, none, 1, st)
-         : p.waves == 4     ? launch<D, 4, 2, 2, Logits::kNone>(a, none, 1, st)
-         : p.kh == 2        ? launch<D, 8, 2, 2, Logits::kNone>(a, none, 1, st)
-         : p.row_groups > 1 ? launch<D, 8, 1, kParts, Logits::kNone, true>(a, none, p.row_groups, st)
-                            : launch<D, 8, 1, kParts, Logits::kNone>(a, none, 1, st);
+  constexpr int kParts = D == 64 ? 2 : 1, kWaves = D == 64 ? 4 : 8;
+  return p.row_groups > 1 ? launch<D, kWaves, 1, kParts, Logits::kNone, true>(a, none, p.row_groups, st)
+                          : launch<D, kWaves, 1, kParts, Logits::kNone>(a, none, 1, st);
 }
 
 }  // namespace

@@ -23,22 +23,30 @@ __global__ __launch_bounds__(256) void join_ranges_kernel(FewRows a) {
 }
 
 constexpr int kMostSplits = 64;
-// Workgroups that the chip holds: one to a compute unit for bf16 at head_dim 128 (LDS), else two.
-int64_t slots_of(int dtype, const Dims& dm) { return dtype == CITRUS_BF16 && dm.D == 128 ? 256 : 512; }
+// Workgroups of a form that the chip holds.
+int64_t slots_of(int dtype, const Dims& dm, const FewRowsPlan& p) {
+  if (dtype == CITRUS_F32) return 512;
+  if (dm.D == 128) return 256;  // LDS
+  return p.waves == 8 ? 256 : p.kh == 1 ? 768 : 512;  // registers, stages in LDS, tiles in LDS
+}
 
+// At head_dim 64 four waves of a block each, three stages in LDS, leave room for three workgroups to a compute unit, of eight waves only one:
+// 16 documents, 16 layers of 8 KV heads, 124 rows over 300 states 97.5 and 60.5 us; 8 KV heads, 3 documents, 427 rows over 14000 states
+// 87 and 100.  Few units of up to 128 rows keep the shorter chain of eight waves that halve a stage (300 states, 13.1 and 14.9).
 FewRowsPlan form_of(int dtype, const Dims& dm, int nodes, bool logits) {
   const int blocks = (dm.G * nodes + 31) / 32;
   FewRowsPlan p{};
   const bool alone = blocks == 1 || logits || dtype == CITRUS_F32;  // a block of 32 rows to a workgroup
-  p.waves = alone || blocks == 2 ? 4 : 8;
-  p.kh = alone ? 4 : blocks <= 4 ? 2 : 1;
+  const bool halves = blocks <= (dm.D == 128 || static_cast<int64_t>(dm.B) * dm.L * dm.Hkv <= 256 ? 4 : 2);
+  p.kh = alone ? 4 : halves ? 2 : 1;
+  p.waves = alone || blocks == 2 || (dm.D == 64 && !halves) ? 4 : 8;
   const int per = p.waves / p.kh;
   p.row_groups = (blocks + per - 1) / per;
   return p;
 }
 int64_t workgroups(const Dims& dm, const FewRowsPlan& p) { return static_cast<int64_t>(dm.B) * dm.L * dm.Hkv * p.row_groups; }
 int most_splits(int dtype, const Dims& dm, const FewRowsPlan& p) {
-  const int64_t s = 8 * slots_of(dtype, dm) / workgroups(dm, p);
+  const int64_t s = 8 * slots_of(dtype, dm, p) / workgroups(dm, p);
   return static_cast<int>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
 }
 
@@ -54,7 +62,7 @@ int most_splits(int dtype, const Dims& dm, const FewRowsPlan& p) {
 // and 1040.
 FewRowsPlan plan_for(int dtype, const Dims& dm, int nodes, int most_keys, bool logits, bool may_evict) {
   FewRowsPlan p = form_of(dtype, dm, nodes, logits);
-  const int64_t groups = workgroups(dm, p), slots = slots_of(dtype, dm);
+  const int64_t groups = workgroups(dm, p), slots = slots_of(dtype, dm, p);
   const int unit = p.kh == 4 ? 32 : 64, tiles = (most_keys + unit - 1) / unit;
   const int rows = dm.G * nodes < 32 * p.waves / p.kh ? dm.G * nodes : 32 * p.waves / p.kh;
   int64_t best = INT64_MAX;
