@@ -7,14 +7,16 @@
 //   private  up to 32: every wave streams 32-key tiles of its own through LDS, with no barrier between the waves; a unit to four waves,
 //            or to one wave where many units have few keys each;
 //   shared   more: the waves of a workgroup read the same 64-key stages, four of them in LDS, a block of 32 rows per KH waves (KH = 2, up
-//            to 128 rows: each takes half of a stage's keys; KH = 1, eight blocks to a workgroup), one barrier a stage.
+//            to 128 rows: each takes half of a stage's keys; KH = 1, eight blocks to a workgroup), one barrier a stage.  At head_dim 64
+//            four blocks to a workgroup and three stages, from 129 rows on, or 65 of more than 256 units: three workgroups then share
+//            a compute unit.
 // Keys are split over workgroups where the units do not fill the chip; another launch joins the ranges.
 // Measured on an MI355X, inputs in turn from three sets: 16 ragged documents, 4 layers of 32/32 heads, head_dim 64, single tokens over up to
 // 2048 states 104.5 us = 6.7 TB/s; 13 nodes, 32/8 heads, 2 layers, over 131072 states 174 us = 6.2 TB/s; 24 nodes, 32 layers of 32/8 heads
 // over 1280 states 40 us = 4.6 TB/s with a start and an end of about 8; 61 nodes, 7 ragged documents, 8 layers of 64/8 heads over up to
 // 4352 states 416 us = 0.66 PFLOP/s, matrix pipe busy 37 % of the SIMD cycles, vector units 43 %: eight waves a compute unit do not
-// cover each other's waits.  There, two tiles a step, 128-key stages, a wave priority around the products, and fewer address instructions
-// changed nothing.  A launch of one tile takes 7.7 us: reads that depend on each other, and instructions that no one has fetched yet.
+// cover each other's waits.  There, two tiles a step, 128-key stages, a wave priority around the products, fewer address instructions, and one wait
+// for all of a tile's reads of LDS changed nothing.  A launch of one tile takes 7.7 us: reads that depend on each other, and instructions that no one has fetched yet.
 #include "evict_unit.h"
 #include "key_stream.h"
 
