@@ -7,9 +7,8 @@
 //   private  up to 32: every wave streams 32-key tiles of its own through LDS, with no barrier between the waves; a unit to four waves,
 //            or to one wave where many units have few keys each;
 //   shared   more: the waves of a workgroup read the same 64-key stages, four of them in LDS, a block of 32 rows per KH waves (KH = 2, up
-//            to 128 rows: each takes half of a stage's keys; KH = 1, eight blocks to a workgroup), one barrier a stage.  At head_dim 64
-//            four blocks to a workgroup and three stages, from 129 rows on, or 65 of more than 256 units: three workgroups then share
-//            a compute unit.
+//            to 128 rows: each takes half of a stage's keys; KH = 1, four or eight blocks to a workgroup), one barrier a stage.  Four
+//            blocks have fewer stages, so that two workgroups share a compute unit, at head_dim 64 three.
 // Keys are split over workgroups where the units do not fill the chip; another launch joins the ranges.
 // Measured on an MI355X, inputs in turn from three sets: 16 ragged documents, 4 layers of 32/32 heads, head_dim 64, single tokens over up to
 // 2048 states 104.5 us = 6.7 TB/s; 13 nodes, 32/8 heads, 2 layers, over 131072 states 174 us = 6.2 TB/s; 24 nodes, 32 layers of 32/8 heads
@@ -28,7 +27,7 @@ typedef __attribute__((address_space(3))) char* lds_char_ptr;
 
 constexpr int kStageKeys = 64;  // shared form
 template <int D, int WAVES, int KH>
-constexpr int kStagesOf = D == 64 && WAVES == 4 && KH == 1 ? 3 : 4;  // three workgroups to a compute unit
+constexpr int kStagesOf = WAVES == 4 && KH == 1 ? (D == 64 ? 3 : 2) : 4;  // three workgroups to a compute unit, two
 constexpr int kLdsOfUnit = 160 * 1024, kLdsOfVote = 1024;  // __syncthreads_and has some of its own, in front of the tiles
 
 // What the lanes of one query row hold of it.
@@ -192,7 +191,7 @@ enum class Logits { kNone, kKept, kEvict, kEvictInLds };
 //
 // GROUPS: several row groups read the same keys.  grid: (row groups * key ranges, Hkv, B * L)
 template <int D, int WAVES, int KH, int PARTS, Logits LOGITS, bool GROUPS>
-__global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 2 : 1) void few_rows_kernel(FewRows a, EvictStep ev) {
+__global__ __launch_bounds__(64 * WAVES, KH == 1 ? 2 : 1) void few_rows_kernel(FewRows a, EvictStep ev) {
   typedef Geo<D> T;
   constexpr bool kPrivate = KH == WAVES;
   constexpr int kBlocks = WAVES / KH;  // of 32 rows
@@ -450,9 +449,13 @@ hipError_t launch_form(const FewRows& a, const FewRowsPlan& p, const EvictStep* 
   if (p.kh == 2) return p.waves == 4 ? launch<D, 4, 2, 2, Logits::kNone>(a, none, 1, st) : launch<D, 8, 2, 2, Logits::kNone>(a, none, 1, st);
   // Two bf16 parts of a weight in P.V cost nothing where the stream of keys bounds; from 129 rows on, at head_dim 128, one: the error of
   // a row is then sqrt(2) times that of the rounding of its result (0.0023 against 0.0017 relative).
-  constexpr int kParts = D == 64 ? 2 : 1, kWaves = D == 64 ? 4 : 8;
-  return p.row_groups > 1 ? launch<D, kWaves, 1, kParts, Logits::kNone, true>(a, none, p.row_groups, st)
-                          : launch<D, kWaves, 1, kParts, Logits::kNone>(a, none, 1, st);
+  constexpr int kParts = D == 64 ? 2 : 1;
+  if constexpr (D == 128)
+    if (p.waves == 8)
+      return p.row_groups > 1 ? launch<D, 8, 1, kParts, Logits::kNone, true>(a, none, p.row_groups, st)
+                              : launch<D, 8, 1, kParts, Logits::kNone>(a, none, 1, st);
+  return p.row_groups > 1 ? launch<D, 4, 1, kParts, Logits::kNone, true>(a, none, p.row_groups, st)
+                          : launch<D, 4, 1, 2, Logits::kNone>(a, none, 1, st);
 }
 
 }  // namespace

@@ -5,6 +5,8 @@
 // over the states j of the row's document: its first len cache rows, then the draft rows that the node's word names.
 #include "few_rows.h"
 
+#include <utility>
+
 namespace citrus {
 namespace {
 
@@ -22,23 +24,27 @@ __global__ __launch_bounds__(256) void join_ranges_kernel(FewRows a) {
   finish_row<E>(a, b, l, h, t, row, d, p, real);
 }
 
-constexpr int kMostSplits = 64;
+constexpr int kMostSplits = 64, kFewKeys = 512;
 // Workgroups of a form that the chip holds.
 int64_t slots_of(int dtype, const Dims& dm, const FewRowsPlan& p) {
-  if (dm.D == 128) return 256;  // LDS, or in f32 registers
+  if (dm.D == 128) return p.waves == 4 && p.kh == 1 ? 512 : 256;  // LDS; in f32 registers
   return dtype == CITRUS_F32 ? 512 : p.waves == 8 ? 256 : p.kh == 1 ? 768 : 512;  // registers, stages in LDS, tiles in LDS
 }
 
-// At head_dim 64 four waves of a block each, three stages in LDS, leave room for three workgroups to a compute unit, of eight waves only one:
-// 16 documents, 16 layers of 8 KV heads, 124 rows over 300 states 97.5 and 60.5 us; 8 KV heads, 3 documents, 427 rows over 14000 states
-// 87 and 100.  Few units of up to 128 rows keep the shorter chain of eight waves that halve a stage (300 states, 13.1 and 14.9).
-FewRowsPlan form_of(int dtype, const Dims& dm, int nodes, bool logits) {
+// More than 64 rows, a block of 32 to a wave: four waves and few stages in LDS leave room for two workgroups to a compute unit, at head_dim
+// 64 for three; eight waves only for one.  head_dim 64: 16 documents, 16 layers of 8 KV heads, 124 rows over 300 states 97.5 and 60.5 us (four
+// waves); 3 documents, 8 KV heads, 427 rows over 14000 states 100 and 87.  head_dim 128: 2560 units of 124 rows over 60, 300, 1200 states 127
+// and 79, 196 and 144, 437 and 394; 288 of them over 4000 states 186 and 171; of 427 rows over 60, 300, 1200 states 326 and 261, 474 and 420,
+// 1012 and 1014, over 4000 states (512 units) 581 and 594; of 160 rows, where half of the second workgroup's waves would have no
+// rows, 136 and 141.  Few units of up to 128 rows keep the shorter chain of eight waves that halve a stage (head_dim 64, 300 states, 13.1 and 14.9).
+FewRowsPlan form_of(int dtype, const Dims& dm, int nodes, int keys, bool logits) {
   const int blocks = (dm.G * nodes + 31) / 32;
   FewRowsPlan p{};
   const bool alone = blocks == 1 || logits || dtype == CITRUS_F32;  // a block of 32 rows to a workgroup
-  const bool halves = blocks <= (dm.D == 128 || static_cast<int64_t>(dm.B) * dm.L * dm.Hkv <= 256 ? 4 : 2);
+  const bool many = static_cast<int64_t>(dm.B) * dm.L * dm.Hkv > 256;
+  const bool halves = blocks <= (many ? 2 : 4), fours = dm.D == 64 || (many && (blocks <= 4 || (blocks > 6 && keys <= kFewKeys)));
   p.kh = alone ? 4 : halves ? 2 : 1;
-  p.waves = alone || blocks == 2 || (dm.D == 64 && !halves) ? 4 : 8;
+  p.waves = alone || blocks == 2 || (fours && !halves) ? 4 : 8;
   const int per = p.waves / p.kh;
   p.row_groups = (blocks + per - 1) / per;
   return p;
@@ -60,7 +66,7 @@ int most_splits(int dtype, const Dims& dm, const FewRowsPlan& p) {
 // 208 and 209, 4000 states 750 and 802; with two heads each and the eviction 81.8 and 30.9, 109 and 57.0, 136 and 94.9, 264 and 265, 962
 // and 1040.
 FewRowsPlan plan_for(int dtype, const Dims& dm, int nodes, int most_keys, bool logits, bool may_evict) {
-  FewRowsPlan p = form_of(dtype, dm, nodes, logits);
+  FewRowsPlan p = form_of(dtype, dm, nodes, most_keys, logits);
   const int64_t groups = workgroups(dm, p), slots = slots_of(dtype, dm, p);
   const int unit = p.kh == 4 ? 32 : 64, tiles = (most_keys + unit - 1) / unit;
   const int rows = dm.G * nodes < 32 * p.waves / p.kh ? dm.G * nodes : 32 * p.waves / p.kh;
@@ -140,9 +146,9 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(Dims dm, View kd, View
 size_t few_rows_workspace_floats(int dtype, const Dims& dm, int rows) {
   size_t most = 0;
   for (int t = 1; t <= rows; ++t)
-    for (const bool logits : {false, true}) {
+    for (const auto& [logits, keys] : {std::pair{false, 0}, {false, kFewKeys + 1}, {true, 0}}) {
       if (logits && t > 1) continue;
-      const int s = most_splits(dtype, dm, form_of(dtype, dm, t, logits));
+      const int s = most_splits(dtype, dm, form_of(dtype, dm, t, keys, logits));
       const size_t f = s == 1 && !logits ? 0 : static_cast<size_t>(s) * dm.B * dm.L * dm.Hq * t * (dm.D + 2);
       if (f > most) most = f;
     }

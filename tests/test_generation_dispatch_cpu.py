@@ -126,6 +126,16 @@ def test_a_unit_to_a_wave_where_many_have_few_keys(tmp_path):
         assert names(launches)[1:] == want[1:]
 
 
+def test_four_waves_of_a_block_each_where_units_are_many(tmp_path):
+    wants = {(1, 64, 32, 8, 128, 24, 130): ("128, 4, 1", 1), (1, 64, 64, 8, 128, 32, 130): ("128, 4, 1", 2), (1, 64, 64, 8, 128, 32, 900): ("128, 8, 1", 1),
+             (1, 64, 64, 8, 128, 20, 130): ("128, 8, 1", 1), (1, 16, 32, 8, 128, 24, 130): ("128, 8, 2", 1), (1, 64, 32, 8, 64, 24, 130): ("64, 4, 1", 1),
+             (1, 16, 64, 8, 64, 32, 70): ("64, 4, 1", 2), (1, 16, 32, 8, 64, 24, 130): ("64, 8, 2", 1)}
+    got = in_child(tree, tmp_path, cases=[[*c, False, -1] for c in wants])
+    for (case, (want, groups)), (status, launches) in zip(wants.items(), got):
+        assert status == 0 and len(launches) == 1 and launches[0][0].startswith(f"few_rows_kernel<{want},"), (case, launches)
+        assert launches[0][1][0] == groups
+
+
 def test_largest_configurations_fit_a_grid(tmp_path):
     """The most heads, the widest groups, and the longest caches that a configuration may have."""
     cases = [[1, 65535, 64, 64, 64, 1, 5, f32, -1] for f32 in (False, True)]

@@ -107,6 +107,26 @@ def test_many_units_of_few_keys(shape):
     same_bits(lse, lse2)
 
 
+MANY_WIDE = [  # ... with more than 64 rows a unit: three, four, seven and eight blocks of 32, few keys and more
+    (1, 130, 8, 2, 128, 24, 70), (2, 65, 16, 2, 128, 16, 0), (1, 130, 8, 2, 128, 56, 200), (2, 65, 16, 2, 128, 31, 130), (1, 130, 8, 2, 128, 60, 600),
+    (1, 130, 8, 2, 64, 24, 70), (1, 130, 8, 2, 64, 64, 33), (1, 130, 8, 2, 64, 40, 300),
+]
+
+
+@pytest.mark.parametrize("shape", MANY_WIDE, ids=lambda s: "x".join(map(str, s)))
+def test_many_units_of_more_rows(shape):
+    case = Case(13, *shape)
+    clean = case.run()
+    case.check(*clean)
+    T = case.T
+    case.words = [[sum(1 << u for u in range(t + 1) if u % 2 == t % 2) for t in range(T)]] * case.cfg.batch
+    clean = case.run()
+    kd, vd = case.kd.clone(), case.vd.clone()
+    kd[:, :, :, 1::2], vd[:, :, :, 1::2] = float("nan"), float("inf")
+    for a, b in zip(_with(case, kd, vd), clean):
+        same_bits(a[:, :, :, 0::2], b[:, :, :, 0::2])
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_many_units_of_few_keys_ragged(d):
     """Documents of other lengths, padding, and a branch whose states are NaN or infinite beside one that does not see them."""
