@@ -342,7 +342,8 @@ int32_t citrus_decode_step(const citrus_config* cfg, citrus_tensor q, citrus_ten
  *                    nearest of these); NULL: cache_len for all.  Rows from a document's length on are not read into its result.
  * lse                optional, dense [B, L, Hq, draft_len] f32: log-sum-exp of each row's scaled logits
  * workspace          >= citrus_generation_workspace_bytes(cfg, draft_len)
- * Compute: as citrus_chunk_attn; row sums in f32.
+ * Compute: bf16 inputs, f32 accumulation and row sums, weights as two bf16 words (together off by 2^-16 of a weight at
+ * most) in the product with V, bf16 output, for every number of nodes and heads; f32 mode computes in f32 throughout.
  */
 int32_t citrus_tree_attn(const citrus_config* cfg, citrus_tensor q, citrus_tensor k_draft, citrus_tensor v_draft, int32_t draft_len,
                          const uint64_t* ancestors, int64_t ancestors_stride_b, citrus_tensor k_cache, citrus_tensor v_cache,
@@ -393,7 +394,8 @@ int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citr
  * recent         1 .. budget - start_size; the same in every step
  * evicted        optional, device, dense int32 [B, L, Hsel]: the row whose state went, -1 while the cache grows
  * workspace      >= citrus_generation_workspace_bytes(cfg, 1)
- * At most 1024 query heads per KV head, else CITRUS_ERR_UNSUPPORTED.  Weights and sums are f32 in both types.
+ * At most 1024 query heads per KV head, else CITRUS_ERR_UNSUPPORTED.  Weights and sums are f32 in both types, out as citrus_tree_attn
+ * computes it.
  */
 int32_t citrus_decode_evict_step(const citrus_config* cfg, citrus_tensor q, citrus_tensor k_new, citrus_tensor v_new,
                                  citrus_tensor k_cache, citrus_tensor v_cache, float* acc, int32_t tokens, int32_t recent,

@@ -28,6 +28,12 @@ typedef __attribute__((address_space(3))) char* lds_char_ptr;
 constexpr int kStageKeys = 64;  // shared form
 template <int D, int WAVES, int KH>
 constexpr int kStagesOf = WAVES == 4 && KH == 1 ? (D == 64 ? 3 : 2) : 4;  // three workgroups to a compute unit, two
+// A weight is two bf16 words in P.V, the second what the first leaves out of the f32 value: together off by 2^-16 of it at most, which
+// is nothing beside the rounding of the result.  With one word the error of a row would be sqrt(2) times that of this rounding, and a
+// row's error has to be the same in every form: which of them serves a tree goes by its number of nodes.  Where the stream of keys bounds
+// the second word costs nothing; beyond 128 rows half as many products more: 320 units of 424 rows over 60, 300, 1200 states 41 and 44, 62
+// and 71, 149 and 183 us.
+constexpr int kWeightParts = 2;
 constexpr int kLdsOfUnit = 160 * 1024, kLdsOfVote = 1024;  // __syncthreads_and has some of its own, in front of the tiles
 
 // What the lanes of one query row hold of it.
@@ -54,8 +60,8 @@ __device__ inline void wait_loads() {
 }
 
 // One 32-key tile.  LAST: keys that not every row sees; bit j of `seen` says that this lane's row sees key j of the tile.
-// PARTS: bf16 words of a weight in P.V.  CAREFUL: see few_rows_kernel.
-template <int D, int PARTS, bool LAST, bool CAREFUL>
+// CAREFUL: see few_rows_kernel.
+template <int D, bool LAST, bool CAREFUL>
 __device__ __forceinline__ void key_tile(uint32_t k_t, uint32_t v_t, const uint32_t (&k_off)[Geo<D>::kKk], const uint32_t (&v_off)[2 * Geo<D>::kOut],
                                          const bf16x8 (&q_op)[Geo<D>::kKk], float c2, uint32_t seen, Column<D>& c, float* scores) {
   typedef Geo<D> T;
@@ -101,14 +107,11 @@ __device__ __forceinline__ void key_tile(uint32_t k_t, uint32_t v_t, const uint3
   float p[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s_acc[i], c2, -m_use));
-  uint32_t p_pk[PARTS][8];
+  uint32_t p_pk[kWeightParts][8];
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if constexpr (PARTS == 2)
-      split_bf16x2(p[2 * i], p[2 * i + 1], p_pk[0][i], p_pk[1][i]);
-    else
-      p_pk[0][i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
+    split_bf16x2(p[2 * i], p[2 * i + 1], p_pk[0][i], p_pk[1][i]);
     sum += p[2 * i] + p[2 * i + 1];
   }
   c.l += sum;
@@ -163,7 +166,7 @@ __device__ __forceinline__ void key_tile(uint32_t k_t, uint32_t v_t, const uint3
       }
     }
 #pragma unroll
-    for (int y = 0; y < PARTS; ++y) {
+    for (int y = 0; y < kWeightParts; ++y) {
       Pack8 pb;
 #pragma unroll
       for (int x = 0; x < 4; ++x) pb.w[x] = p_pk[y][4 * half + x];
@@ -190,7 +193,7 @@ enum class Logits { kNone, kKept, kEvict, kEvictInLds };
 // values; a workgroup whose results are not all finite goes over its keys once more, carefully.
 //
 // GROUPS: several row groups read the same keys.  grid: (row groups * key ranges, Hkv, B * L)
-template <int D, int WAVES, int KH, int PARTS, Logits LOGITS, bool GROUPS>
+template <int D, int WAVES, int KH, Logits LOGITS, bool GROUPS>
 __global__ __launch_bounds__(64 * WAVES, KH == 1 ? 2 : 1) void few_rows_kernel(FewRows a, EvictStep ev) {
   typedef Geo<D> T;
   constexpr bool kPrivate = KH == WAVES;
@@ -301,7 +304,7 @@ __global__ __launch_bounds__(64 * WAVES, KH == 1 ? 2 : 1) void few_rows_kernel(F
     // Tiles of cached states that every row sees come first.  (Apart from the others, in a loop of their own: where the two met in one
     // loop, the accumulators went from one set of registers to another and back with every tile.)
     auto tile = [&]<bool LAST>(int j0, uint32_t k_t, uint32_t v_t) {
-      key_tile<D, PARTS, LAST, CAREFUL>(k_t, v_t, k_off, v_off, q_op, c2, LAST ? seen_keys(word, j0 - n_c) : 0u, c,
+      key_tile<D, LAST, CAREFUL>(k_t, v_t, k_off, v_off, q_op, c2, LAST ? seen_keys(word, j0 - n_c) : 0u, c,
                                         LOGITS != Logits::kNone && scores != nullptr ? scores + j0 : nullptr);
     };
     if constexpr (kPrivate) {
@@ -418,12 +421,12 @@ __global__ __launch_bounds__(64 * WAVES, KH == 1 ? 2 : 1) void few_rows_kernel(F
   }
 }
 
-template <int D, int WAVES, int KH, int PARTS, Logits LOGITS, bool GROUPS = false>
+template <int D, int WAVES, int KH, Logits LOGITS, bool GROUPS = false>
 hipError_t launch(const FewRows& a, const EvictStep& ev, int row_groups, hipStream_t st) {
   typedef Lds<D, WAVES, KH> L;
   const int strip = LOGITS == Logits::kEvictInLds ? a.dm.G * strip_pitch(ev.n) * 4 : 0;
   static LdsLimit limit;
-  const auto kernel = few_rows_kernel<D, WAVES, KH, PARTS, LOGITS, GROUPS>;
+  const auto kernel = few_rows_kernel<D, WAVES, KH, LOGITS, GROUPS>;
   const hipError_t e = raise_lds_limit(limit, reinterpret_cast<const void*>(kernel), LOGITS == Logits::kEvictInLds ? kLdsOfUnit - kLdsOfVote : L::kBytes);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(kernel, dim3(row_groups * a.splits, a.dm.Hkv, a.dm.B * a.dm.L), dim3(64 * WAVES), L::kBytes + strip, st, a, ev);
@@ -433,29 +436,26 @@ template <int D>
 hipError_t launch_form(const FewRows& a, const FewRowsPlan& p, const EvictStep* ev, hipStream_t st) {
   const EvictStep none{};
   if (p.waves == 1)  // a unit to a wave; its logits, if any, in the workspace: a strip of them in LDS costs waves
-    return ev == nullptr ? launch<D, 1, 1, 2, Logits::kNone>(a, none, 1, st)
-           : p.evicts    ? launch<D, 1, 1, 2, Logits::kEvict>(a, *ev, 1, st)
-                         : launch<D, 1, 1, 2, Logits::kKept>(a, none, 1, st);
+    return ev == nullptr ? launch<D, 1, 1, Logits::kNone>(a, none, 1, st)
+           : p.evicts    ? launch<D, 1, 1, Logits::kEvict>(a, *ev, 1, st)
+                         : launch<D, 1, 1, Logits::kKept>(a, none, 1, st);
   if (ev != nullptr) {
     // the strip lies in LDS where that leaves as many workgroups to a compute unit as there are without it
     const int units = D == 128 ? 1 : 2;
     const bool fits = a.dm.G * strip_pitch(ev->n) * 4 + Lds<D, 4, 4>::kBytes <= kLdsOfUnit / units - kLdsOfVote;
     if (!p.evicts)
-      return p.row_groups > 1 ? launch<D, 4, 4, 2, Logits::kKept, true>(a, none, p.row_groups, st)
-                              : launch<D, 4, 4, 2, Logits::kKept>(a, none, 1, st);
-    return fits ? launch<D, 4, 4, 2, Logits::kEvictInLds>(a, *ev, 1, st) : launch<D, 4, 4, 2, Logits::kEvict>(a, *ev, 1, st);
+      return p.row_groups > 1 ? launch<D, 4, 4, Logits::kKept, true>(a, none, p.row_groups, st)
+                              : launch<D, 4, 4, Logits::kKept>(a, none, 1, st);
+    return fits ? launch<D, 4, 4, Logits::kEvictInLds>(a, *ev, 1, st) : launch<D, 4, 4, Logits::kEvict>(a, *ev, 1, st);
   }
-  if (p.kh == 4) return launch<D, 4, 4, 2, Logits::kNone>(a, none, 1, st);
-  if (p.kh == 2) return p.waves == 4 ? launch<D, 4, 2, 2, Logits::kNone>(a, none, 1, st) : launch<D, 8, 2, 2, Logits::kNone>(a, none, 1, st);
-  // Two bf16 parts of a weight in P.V cost nothing where the stream of keys bounds; from 129 rows on, at head_dim 128, one: the error of
-  // a row is then sqrt(2) times that of the rounding of its result (0.0023 against 0.0017 relative).
-  constexpr int kParts = D == 64 ? 2 : 1;
+  if (p.kh == 4) return launch<D, 4, 4, Logits::kNone>(a, none, 1, st);
+  if (p.kh == 2) return p.waves == 4 ? launch<D, 4, 2, Logits::kNone>(a, none, 1, st) : launch<D, 8, 2, Logits::kNone>(a, none, 1, st);
   if constexpr (D == 128)
     if (p.waves == 8)
-      return p.row_groups > 1 ? launch<D, 8, 1, kParts, Logits::kNone, true>(a, none, p.row_groups, st)
-                              : launch<D, 8, 1, kParts, Logits::kNone>(a, none, 1, st);
-  return p.row_groups > 1 ? launch<D, 4, 1, kParts, Logits::kNone, true>(a, none, p.row_groups, st)
-                          : launch<D, 4, 1, 2, Logits::kNone>(a, none, 1, st);
+      return p.row_groups > 1 ? launch<D, 8, 1, Logits::kNone, true>(a, none, p.row_groups, st)
+                              : launch<D, 8, 1, Logits::kNone>(a, none, 1, st);
+  return p.row_groups > 1 ? launch<D, 4, 1, Logits::kNone, true>(a, none, p.row_groups, st)
+                          : launch<D, 4, 1, Logits::kNone>(a, none, 1, st);
 }
 
 }  // namespace
