@@ -92,16 +92,18 @@ __device__ __forceinline__ void key_tile(uint32_t k_t, uint32_t v_t, const uint3
   float mx = s_acc[0];
 #pragma unroll
   for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s_acc[i]);
-  if (__any(mx * c2 > c.m + kMaxSlack)) {  // the maximum moves only when some row's did by more than that
+  if (__any(mx * c2 > c.m + kMaxSlack)) {
+    // A row's maximum moves only by more than that, and only by what the row sees: moved along with a neighbour's, it would have its weights
+    // rounded otherwise, for keys or queries that are not the row's.
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float m_new = fmaxf(c.m, mx * c2);
-    const float alpha = __builtin_amdgcn_exp2f(c.m - (m_new == -INFINITY ? 0.f : m_new));  // 0 on the first tile
+    const bool moves = mx * c2 > c.m + kMaxSlack;
+    const float alpha = moves ? __builtin_amdgcn_exp2f(c.m - mx * c2) : 1.f;  // 0 on the first tile
+    c.m = moves ? mx * c2 : c.m;
     c.l *= alpha;
 #pragma unroll
     for (int r = 0; r < T::kOut; ++r)
 #pragma unroll
       for (int i = 0; i < 16; ++i) c.o[r][i] *= alpha;
-    c.m = m_new;
   }
   const float m_use = LAST && c.m == -INFINITY ? 0.f : c.m;  // a row that has not seen a state yet
   float p[16];

@@ -46,3 +46,41 @@ def test_rows_are_as_exact_whatever_form_serves_them(shape, dtype):
         ref, _, mag = orc.tree_attn(q, kd, vd, case.words[0], kc, vc)
         off, most = np.abs(got - ref), bound(ref, mag, case.n + case.T, dtype)
         assert (off <= most).all(), f"layer {l}: {(off > most).sum()} of {off.size} outside, worst {np.max(off / most):.3g} of its bound"
+
+
+SEVERAL_TILES = [  # ... to a wave, in every form: the reference that a row's weights are formed against may lag behind its maximum
+    (1, 140, 8, 2, 128, 6, 200), (1, 128, 4, 2, 128, 6, 700), (1, 1, 8, 1, 128, 8, 700), (1, 1, 8, 1, 128, 14, 700), (1, 1, 8, 1, 128, 25, 700),
+    (1, 1, 8, 1, 128, 64, 700), (1, 130, 8, 2, 128, 24, 150), (1, 130, 8, 2, 128, 56, 150), (1, 140, 8, 2, 64, 6, 200), (1, 128, 4, 2, 64, 6, 700),
+    (1, 1, 8, 1, 64, 14, 700), (1, 1, 8, 1, 64, 25, 700), (1, 1, 8, 1, 64, 64, 700), (1, 130, 8, 2, 64, 24, 150),
+]
+
+
+def _same_rows(a, b, rows, what):
+    for x, y in zip(a, b):
+        x, y = x[:, :, :, rows].contiguous(), y[:, :, :, rows].contiguous()
+        kind = torch.int16 if x.dtype == torch.bfloat16 else torch.int32
+        differ = int((x.view(kind) != y.view(kind)).sum())
+        assert differ == 0, f"{what}: {differ} of {x.numel()} values differ"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SEVERAL_TILES, ids=lambda s: "x".join(map(str, s)))
+def test_a_row_depends_on_nothing_but_what_it_sees(shape, dtype):
+    """Large and infinite keys that a node does not see, large queries of other nodes and of padding: its row keeps its bits."""
+    case = Case(42, *shape, dtype=dtype)
+    T = case.T
+    left, right = list(range(0, T, 2)), list(range(1, T, 2))
+    branches = [sum(1 << u for u in range(t + 1) if u % 2 == t % 2) for t in range(T)]
+    case.words = [branches]
+    clean, keys, queries = case.run(), case.kd.clone(), case.q.clone()
+    case.kd[:, :, :, right] *= 50
+    _same_rows(case.run(), clean, left, "large unseen keys")
+    case.kd[:, :, :, right, 3] = float("inf")
+    _same_rows(case.run(), clean, left, "unseen keys with an infinite element")
+    case.kd.copy_(keys)
+    case.q[:, :, :, right] *= 40
+    _same_rows(case.run(), clean, left, "large queries of other nodes")
+    case.words = [[w if t % 2 == 0 else 0 for t, w in enumerate(branches)]]
+    for factor in (1.0, 100.0, float("inf")):
+        case.q[:, :, :, right] = (queries[:, :, :, right] * factor).nan_to_num(1.0, float("inf"), float("-inf"))
+        _same_rows(case.run(), clean, left, f"padding, queries times {factor}")
