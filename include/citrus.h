@@ -355,7 +355,8 @@ int32_t citrus_tree_attn(const citrus_config* cfg, citrus_tensor q, citrus_tenso
  *   cache row len_b + i = draft row path[b, i]     of K and of V, in every layer and head; bit copies.
  * Rows from len_b + accepted[b] on are left as they were.
  *
- * k_draft, v_draft   [B, L, Hkv, draft_len, d]; 1 <= draft_len <= 64; must not overlap the caches
+ * k_draft, v_draft   [B, L, Hkv, draft_len, d]; 1 <= draft_len <= 64; must not overlap the caches' cache_capacity rows, wherever
+ *                    citrus_tree_attn read them (a view of these rows: CITRUS_ERR_SHAPE)
  * path               device, dense int32 [B, path_len]: node numbers 0 .. draft_len - 1 from the root on; 1 <= path_len <= 64.  A
  *                    number outside leaves its cache row as it was.
  * accepted           device int32 [B], 0 .. path_len (values outside are taken as the nearest of these; no row is written
@@ -385,8 +386,9 @@ int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citr
  * depend on the order of its states.)  With start_size + recent == budget this is a sliding window behind the first states.
  * cfg->select_mode PER_LAYER: one row for all KV heads of a layer, by the sum of their sums in head order.
  *
- * q, out         [B, L, Hq, 1, d];  k_new, v_new  [B, L, Hkv, 1, d]: the token's own state, not in the caches' memory; out must not
- *                overlap an input
+ * q, out         [B, L, Hq, 1, d];  k_new, v_new  [B, L, Hkv, 1, d]: the token's own state, in none of the caches' first
+ *                min(tokens + 1, budget) rows (a view of these: CITRUS_ERR_SHAPE), but that while the cache grows it may lie in the
+ *                row that becomes its own; out must not overlap an input
  * k_cache, v_cache [B, L, Hkv, >= min(tokens + 1, budget), d], in/out
  * acc            dense f32 [B, L, Hkv, cache_capacity], in/out: the states' sums
  * tokens         states that have been put into this cache so far, evicted ones included; the caller's count becomes tokens + 1.  A

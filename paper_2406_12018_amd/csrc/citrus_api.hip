@@ -5,6 +5,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include "citrus_internal.h"
 
 using namespace citrus;
@@ -410,6 +412,59 @@ citrus_status check_generation_workspace(const citrus_config* c, int draft_len, 
   if (reinterpret_cast<uintptr_t>(ws) % 16 != 0) return CITRUS_ERR_WORKSPACE;
   return CITRUS_OK;
 }
+// Do rows 0 .. rows_a - 1 of a and 0 .. rows_b - 1 of b, both of `kv_heads` heads, lie on the same memory somewhere?  Answered where one is a
+// view of the other's rows, i.e. where their strides are the same (an axis of one element has none): a combination of the axes' index
+// differences is looked for whose addresses are less than a row apart, the longest axis first, only as far as the shorter ones reach.
+bool share_rows(const citrus_config* c, const citrus_tensor& a, int rows_a, const citrus_tensor& b, int rows_b) {
+  struct Axis {
+    int64_t bytes;
+    int64_t least, most;  // index in b less index in a
+  };
+  Axis axes[4];
+  int n = 0;
+  const int esz = elem_bytes(c->dtype);
+  const auto add = [&](int64_t in_a, int64_t in_b, int count_a, int count_b) {
+    if (count_a > 1 && count_b > 1 && in_a != in_b) return false;
+    const int64_t stride = (count_a > 1 ? in_a : in_b) * esz;
+    if ((count_a > 1 || count_b > 1) && stride != 0)
+      axes[n++] = stride > 0 ? Axis{stride, 1 - count_a, count_b - 1} : Axis{-stride, 1 - count_b, count_a - 1};
+    return true;
+  };
+  if (rows_a < 1 || rows_b < 1 || !add(a.stride_b, b.stride_b, c->batch, c->batch) || !add(a.stride_l, b.stride_l, c->layers, c->layers) ||
+      !add(a.stride_h, b.stride_h, c->kv_heads, c->kv_heads) || !add(a.stride_s, b.stride_s, rows_a, rows_b))
+    return false;
+  std::sort(axes, axes + n, [](const Axis& x, const Axis& y) { return x.bytes > y.bytes; });
+  typedef __int128 Wide;  // strides of axes are not bounded
+  Wide up[5] = {}, down[5] = {};  // how far the axes from i on reach
+  for (int i = n; i-- > 0;) {
+    up[i] = up[i + 1] + static_cast<Wide>(axes[i].bytes) * axes[i].most;
+    down[i] = down[i + 1] - static_cast<Wide>(axes[i].bytes) * axes[i].least;
+  }
+  const Wide row = static_cast<Wide>(c->head_dim) * esz;
+  int looks = 4096;  // enough for layouts whose own rows are apart: they leave three differences an axis at most
+  const auto meet = [&](const auto& self, int i, Wide apart) -> bool {
+    if (apart + up[i] <= -row || apart - down[i] >= row || --looks < 0) return false;
+    if (i == n) return true;
+    const Wide s = axes[i].bytes;
+    const Wide first = (-row - up[i + 1] - apart) / s - 1, last = (row + down[i + 1] - apart) / s + 1;
+    for (Wide x = first < axes[i].least ? axes[i].least : first; x <= last && x <= axes[i].most && looks > 0; ++x)
+      if (self(self, i + 1, apart + x * s)) return true;
+    return false;
+  };
+  return meet(meet, 0, static_cast<Wide>(reinterpret_cast<intptr_t>(b.ptr)) - reinterpret_cast<intptr_t>(a.ptr));
+}
+// Does a state that joins the caches lie in their first rows?  (`behind`: in row rows - 1 its own place is none of them: the copy that
+// puts it there changes nothing.)
+bool in_the_caches(const citrus_config* c, const citrus_tensor& k_cache, const citrus_tensor& v_cache, int rows, const citrus_tensor& k,
+                   const citrus_tensor& v, int states, bool behind) {
+  const auto in_place = [&](const citrus_tensor& cache, const citrus_tensor& t) {
+    return behind && t.ptr == rows_from(cache, rows - 1, c->dtype).ptr && (c->batch == 1 || t.stride_b == cache.stride_b) &&
+           (c->layers == 1 || t.stride_l == cache.stride_l) && (c->kv_heads == 1 || t.stride_h == cache.stride_h);
+  };
+  return (!in_place(k_cache, k) && (k.ptr == k_cache.ptr || share_rows(c, k_cache, rows, k, states))) ||
+         (!in_place(v_cache, v) && (v.ptr == v_cache.ptr || share_rows(c, v_cache, rows, v, states))) ||
+         share_rows(c, k_cache, rows, v, states) || share_rows(c, v_cache, rows, k, states);
+}
 template <typename T>
 bool misaligned(const T* p) { return reinterpret_cast<uintptr_t>(p) % sizeof(T) != 0; }
 citrus_status check_draft(const citrus_config* c, int draft_len, int cache_len, const citrus_tensor& k_draft, const citrus_tensor& v_draft,
@@ -625,6 +680,7 @@ int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citr
   if (path_len < 1 || path_len > kMaxNodes || misaligned(path) || misaligned(accepted) || misaligned(new_lens)) return CITRUS_ERR_SHAPE;
   CITRUS_TRY(check_tensor(cfg, k_cache, cfg->cache_capacity, false));
   CITRUS_TRY(check_tensor(cfg, v_cache, cfg->cache_capacity, false));
+  if (in_the_caches(cfg, k_cache, v_cache, cfg->cache_capacity, k_draft, v_draft, draft_len, false)) return CITRUS_ERR_SHAPE;
   if (new_lens != nullptr && (new_lens == cache_lens || new_lens == accepted || new_lens == path)) return CITRUS_ERR_SHAPE;
   const Commit a{path, accepted, cache_lens, new_lens, path_len, draft_len, cache_len, cfg->cache_capacity, fast_div(cfg->layers)};
   return hip_status(launch_tree_commit(elem_bytes(cfg->dtype), dims_of(cfg), make_view(k_draft), make_view(v_draft), make_view(k_cache),
@@ -647,7 +703,7 @@ int32_t citrus_decode_evict_step(const citrus_config* cfg, citrus_tensor q, citr
   CITRUS_TRY(check_tensor(cfg, k_cache, rows, false));
   CITRUS_TRY(check_tensor(cfg, v_cache, rows, false));
   CITRUS_TRY(check_tensor(cfg, out, 1, false));
-  if (k_new.ptr == k_cache.ptr || v_new.ptr == v_cache.ptr || out.ptr == q.ptr) return CITRUS_ERR_SHAPE;
+  if (out.ptr == q.ptr || in_the_caches(cfg, k_cache, v_cache, rows, k_new, v_new, 1, !full)) return CITRUS_ERR_SHAPE;
   CITRUS_TRY(check_generation_workspace(cfg, 1, workspace, workspace_bytes));
   const EvictStepLayout wl = evict_step_layout(cfg);
   char* ws = static_cast<char*>(workspace);

@@ -131,6 +131,29 @@ def test_the_binding_refuses_tensors_that_do_not_fit(monkeypatch):
         api.citrus_decode_evict_step(c, **{**evict_args, "recent": 65}, stream=0)
 
 
+ROW = 64 * 4
+
+
+@pytest.mark.parametrize("kw", [
+    dict(kd=at(0x5000 + 16 * ROW)), dict(vd=at(0x6000 + 16 * ROW)),          # behind the cached rows, where a draft may be read
+    dict(kd=at(0x5000 + 60 * ROW)), dict(kd=at(0x5000 - 7 * ROW)),           # its first rows in the cache, its last one
+    dict(kd=at(0x6000 + 2 * ROW), vc=at(0x6000)), dict(vd=at(0x5000 + 63 * ROW)),  # K in V's cache and the other way
+    dict(kd=at(0x5000 + 0x8000 + 30 * ROW)), dict(vd=at(0x6000 + 0x40000 + 1)),   # of the next head, of the next document
+    dict(kd=at(0x5000 - 0x8000 + 30 * ROW)),
+])
+def test_a_commit_refuses_a_view_of_the_cache(kw):
+    kw = {k: B.CTensor(t.ptr // 16 * 16, t.stride_b, t.stride_l, t.stride_h, t.stride_s) for k, t in kw.items()}
+    assert commit(**kw) == B.ERR_SHAPE
+
+
+@pytest.mark.parametrize("kw", [
+    dict(kn=at(0x5000 + 16 * ROW)), dict(vn=at(0x6000 + 63 * ROW)), dict(kn=at(0x6000 + 5 * ROW)), dict(vn=at(0x5000 + 5 * ROW)),
+    dict(tokens=20, kn=at(0x5000 + 19 * ROW)), dict(tokens=20, vn=at(0x5000 + 20 * ROW)), dict(tokens=20, kn=at(0x5000 + 0x8000 + 20 * ROW)),
+])
+def test_bounded_decoding_refuses_a_view_of_the_cached_states(kw):
+    assert evict(**kw) == B.ERR_SHAPE
+
+
 # ---- pins of the oracle ----
 def test_a_chain_is_causal_attention_and_a_step_a_decoding_step():
     rng = np.random.default_rng(1)

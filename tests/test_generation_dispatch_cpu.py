@@ -82,6 +82,36 @@ def evict(api, launches, cases):
     return out
 
 
+def joins(api, launches, cases):
+    """Calls whose new states lie beside the caches' rows or in their own place: the launches of each."""
+    make, torch = fakes(api)
+    dtype, out = torch.float32, []
+    L, H, cap, T, d, ROW = 3, 4, 64, 8, 64, 256
+
+    def view(at, **kw):  # [2, L, H, rows, d] with the strides of a cache, in bytes
+        st = {**dict(b=L * H * 80 * ROW, l=H * 80 * ROW, h=80 * ROW, s=ROW), **kw}
+        return api.binding.CTensor(at, *(st[x] // 4 for x in "blhs"))
+
+    cfg = api.Config(batch=2, layers=L, q_heads=H, kv_heads=H, head_dim=d, chunk_len=1, budget=cap, instr_len=1, dtype=api.F32, cache_capacity=cap)
+    lib, cc, kc, vc, apart = api.binding._lib(), cfg.c(), 1 << 24, 2 << 24, 5 << 24
+    for kind, k_at, v_at, tokens, interleaved in cases:
+        kw = dict(s=3 * ROW, h=80 * 3 * ROW, l=H * 80 * 3 * ROW, b=L * H * 80 * 3 * ROW) if interleaved else {}
+        kc_t, vc_t = view(kc, **kw), view(kc + 2 * ROW if interleaved else vc, **kw)
+        k, v = (view(apart + i * (1 << 24) if x is None else x, **kw) for i, x in enumerate((k_at, v_at)))
+        status = [0]
+
+        def call():
+            if kind == "commit":
+                status[0] = lib.citrus_tree_commit(C.byref(cc), k, v, T, 1 << 30, 4, 1 << 31, kc_t, vc_t, 16, None, None, None)
+            else:
+                status[0] = lib.citrus_decode_evict_step(C.byref(cc), view(8 << 24), k, v, kc_t, vc_t, 1 << 30, tokens, 1, view(9 << 24), None,
+                                                         1 << 32, 1 << 40, None)
+
+        got = [x for x in launches(call) if x[0] != "lds"]
+        out.append([status[0], len(got)])
+    return out
+
+
 # ---- in the test ----
 def in_child(body, tmp_path, **kw):
     shim = str(tmp_path / "fake_hip.so")
@@ -161,6 +191,19 @@ def test_forms_of_the_eviction(tmp_path):
     got = in_child(evict, tmp_path, cases=[[*c, -1] for c in wants])
     for (case, want), (status, launches) in zip(wants.items(), got):
         assert status == 0 and names(launches) == want, (case, launches)
+
+
+def test_states_beside_the_cached_rows_are_taken(tmp_path):
+    """Memory that K, V and drafts share row by row, rows behind the capacity, and a token in the row that becomes its own."""
+    ROW, kc, vc = 256, 1 << 24, 2 << 24
+    cases = [["commit", None, None, 0, False], ["commit", kc + 64 * ROW, vc + 64 * ROW, 0, False], ["commit", kc - 8 * ROW, vc + 64 * ROW, 0, False],
+             ["commit", kc + ROW, None, 0, True], ["commit", None, kc + 3 * ROW * 70 + 2 * ROW, 0, True], ["evict", None, None, 70, False], ["evict", kc + 64 * ROW, vc + 64 * ROW, 70, False],
+             ["evict", kc + 20 * ROW, vc + 20 * ROW, 20, False], ["evict", kc, vc, 0, False], ["evict", kc + ROW, None, 70, True]]
+    refused = [["commit", kc + 56 * ROW, None, 0, False], ["commit", kc + 3 * ROW * 20, None, 0, True],
+               ["evict", kc + 63 * ROW, None, 70, False], ["evict", vc + 20 * ROW, kc + 20 * ROW, 20, False]]
+    got = in_child(joins, tmp_path, cases=cases + refused)
+    assert all(status == 0 and launches for status, launches in got[:len(cases)]), got
+    assert all(x == [2, 0] for x in got[len(cases):]), got
 
 
 def test_failed_launches_are_reported(tmp_path):

@@ -185,6 +185,18 @@ def test_sums_that_are_no_numbers():
     assert (run.evicted == 30).all()
 
 
+@pytest.mark.parametrize("name", ["window", "tile_edges", "per_layer", "many_heads"])
+def test_a_token_in_the_row_that_becomes_its_own(name):
+    """While the cache grows the token's state may be written there before the step; the bits are those of one that comes from elsewhere."""
+    a, b = (Run(95, **CASES[name]) for _ in range(2))
+    for n in range(a.cfg.budget):
+        q, k, v = a.token()
+        b.k[:, :, :, n:n + 1], b.v[:, :, :, n:n + 1] = k, v
+        same_bits(a.call(q, k, v), b.call(q, b.k[:, :, :, n:n + 1], b.v[:, :, :, n:n + 1]))
+        for x, y in ((a.k, b.k), (a.v, b.v), (a.acc, b.acc)):
+            same_bits(x, y)
+
+
 @pytest.mark.parametrize("name", ["one_layer", "long", "many_units", "long_per_layer"])
 def test_captured_steps_replay(name):
     """Three steps in a graph; every replay, from the same start, leaves the bits that eager steps leave."""
