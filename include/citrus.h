@@ -342,6 +342,9 @@ int32_t citrus_decode_step(const citrus_config* cfg, citrus_tensor q, citrus_ten
  *                    nearest of these); NULL: cache_len for all.  Rows from a document's length on are not read into its result.
  * lse                optional, dense [B, L, Hq, draft_len] f32: log-sum-exp of each row's scaled logits
  * workspace          >= citrus_generation_workspace_bytes(cfg, draft_len)
+ * With cfg->position_shift the caches hold keys without rotation, and the call refuses (CITRUS_ERR_UNSUPPORTED): rotate the
+ * queries, the draft's keys and a copy of the cached ones (citrus_rope) and pass a configuration without it.  citrus_tree_commit copies
+ * keys of either kind.
  * Compute: bf16 inputs, f32 accumulation and row sums, weights as two bf16 words (together off by 2^-16 of a weight at
  * most) in the product with V, bf16 output, for every number of nodes and heads; f32 mode computes in f32 throughout.
  */
@@ -396,6 +399,8 @@ int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citr
  * recent         1 .. budget - start_size; the same in every step
  * evicted        optional, device, dense int32 [B, L, Hsel]: the row whose state went, -1 while the cache grows
  * workspace      >= citrus_generation_workspace_bytes(cfg, 1)
+ * With cfg->position_shift, where a state's position is its row, CITRUS_ERR_UNSUPPORTED: states change rows here, and their keys carry
+ * their rotation.
  * At most 1024 query heads per KV head, else CITRUS_ERR_UNSUPPORTED.  Weights and sums are f32 in both types, out as citrus_tree_attn
  * computes it.
  */

@@ -648,6 +648,7 @@ int32_t citrus_tree_attn(const citrus_config* cfg, citrus_tensor q, citrus_tenso
                          int32_t cache_len, const int32_t* cache_lens, citrus_tensor out, float* lse, void* workspace,
                          size_t workspace_bytes, void* hip_stream) {
   CITRUS_TRY(check_config(cfg));
+  if (cfg->position_shift) return CITRUS_ERR_UNSUPPORTED;  // the caches' keys are not rotated
   CITRUS_TRY(check_draft(cfg, draft_len, cache_len, k_draft, v_draft, k_cache, v_cache, cache_lens, false));
   if (ancestors == nullptr) return CITRUS_ERR_NULL;
   if (misaligned(ancestors) || misaligned(lse) || (ancestors_stride_b != 0 && ancestors_stride_b < draft_len)) return CITRUS_ERR_SHAPE;
@@ -692,7 +693,7 @@ int32_t citrus_decode_evict_step(const citrus_config* cfg, citrus_tensor q, citr
                                  citrus_tensor out, int32_t* evicted, void* workspace, size_t workspace_bytes, void* hip_stream) {
   CITRUS_TRY(check_config(cfg));
   if (tokens < 0 || recent < 1 || recent > cfg->budget - cfg->start_size) return CITRUS_ERR_SHAPE;
-  if (cfg->q_heads / cfg->kv_heads > 1024) return CITRUS_ERR_UNSUPPORTED;
+  if (cfg->position_shift || cfg->q_heads / cfg->kv_heads > 1024) return CITRUS_ERR_UNSUPPORTED;
   if (acc == nullptr) return CITRUS_ERR_NULL;
   if (misaligned(acc) || misaligned(evicted)) return CITRUS_ERR_SHAPE;
   const bool full = tokens >= cfg->budget;

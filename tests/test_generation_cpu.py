@@ -131,6 +131,14 @@ def test_the_binding_refuses_tensors_that_do_not_fit(monkeypatch):
         api.citrus_decode_evict_step(c, **{**evict_args, "recent": 65}, stream=0)
 
 
+def test_caches_of_unrotated_keys_are_refused():
+    """With position_shift the caches hold keys without rotation: no attention over them as they are.  The commit copies any."""
+    shift = cfg(position_shift=1).c()
+    assert tree(c=shift) == B.ERR_UNSUPPORTED and evict(c=shift) == B.ERR_UNSUPPORTED
+    assert commit(c=shift, path=None) == B.ERR_NULL
+    assert api.generation_workspace_bytes(cfg(position_shift=1), 8) == api.generation_workspace_bytes(cfg(), 8)
+
+
 ROW = 64 * 4
 
 
