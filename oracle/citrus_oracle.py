@@ -585,7 +585,8 @@ def decode_evict_step(q_new, k_new, v_new, k_cache, v_cache, acc, tokens: int, b
     Section 5.2 "Baselines", during generation).
 
     q_new [Hq, d], k_new / v_new [Hkv, d]; k_cache / v_cache [Hkv, n, d] and acc [Hkv, n] with n = min(tokens, budget).
-    forced: the row to evict per KV head (a caller replays another selection), else the smallest sum, the lowest row of equal ones.
+    forced: the row to evict per KV head (a caller replays another selection), else the smallest sum, the lowest row of equal ones.  A
+    sum that is NaN is never the smallest; the oldest recent row goes if there is no smaller one.
     Returns (out [Hq, d], sums [Hkv, n + 1] before anything moves, evicted rows per KV head or None, k, v, acc after the step).
     """
     q_new, k_new, v_new, k_cache, v_cache, acc = (_f64(x) for x in (q_new, k_new, v_new, k_cache, v_cache, acc))
@@ -607,10 +608,10 @@ def decode_evict_step(q_new, k_new, v_new, k_cache, v_cache, acc, tokens: int, b
     evicted = np.zeros(hkv, dtype=np.int64)
     k_after, v_after, acc_after = k[:, :n].copy(), v[:, :n].copy(), sums[:, :n].copy()
     for g in range(hkv):
-        best = oldest
-        for j in list(range(start_size, budget - recent)) + [oldest]:
-            if rank[g, j] < rank[g, best] or (rank[g, j] == rank[g, best] and j < best):
-                best = j
+        best, least = oldest, np.inf if np.isnan(rank[g, oldest]) else rank[g, oldest]
+        for j in range(start_size, budget - recent):  # the rows before it
+            if rank[g, j] < least or (rank[g, j] == least and j < best):
+                best, least = j, rank[g, j]
         evicted[g] = best if forced is None else forced[g]
         for dst, src in ((evicted[g], oldest), (oldest, n)):
             k_after[g, dst], v_after[g, dst], acc_after[g, dst] = k[g, src], v[g, src], sums[g, src]

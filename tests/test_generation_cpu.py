@@ -189,6 +189,17 @@ def test_a_window_keeps_the_first_and_the_newest_states():
     assert left == [0, 1, 37, 38, 39]
 
 
+def test_a_sum_that_is_no_number_is_never_the_smallest():
+    """Of the oldest recent state (row 3) neither; where no other is smaller it goes."""
+    nan, inf, k = float("nan"), float("inf"), np.zeros((1, 5, 2))
+    for acc, row in (([9.0, 2.0, 3.0, nan, 1.0], 1), ([nan, 7.0, nan, nan, 1.0], 1), ([nan, nan, nan, nan, 0.0], 3), ([nan, nan, nan, 5.0, 0.0], 3),
+                     ([nan, 4.0, 4.0, 5.0, 0.0], 1), ([inf, inf, nan, nan, 0.0], 0), ([9.0, 9.0, 9.0, 9.0, 0.0], 0)):
+        for mode in (orc.SELECT_PER_KV_HEAD, orc.SELECT_PER_LAYER):
+            _, _, gone, _, _, _ = orc.decode_evict_step(np.zeros((1, 2)), np.zeros((1, 2)), np.zeros((1, 2)), k, k, np.array([acc]), 5, 5, 2,
+                                                        select_mode=mode)
+            assert gone[0] == row, (acc, gone)
+
+
 def test_the_least_attended_state_goes_and_the_oldest_recent_one_takes_its_row():
     k = np.array([[[4.0], [0.0], [-9.0], [1.0], [2.0]]])  # 4 of 5 rows may go with recent = 2: 0 .. 2 and the older recent one
     _, sums, gone, after, _, acc = orc.decode_evict_step([[1.0]], [[0.5]], [[0.5]], k, k, np.zeros((1, 5)), 5, 5, 2, scale=1.0)
