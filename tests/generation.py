@@ -64,3 +64,78 @@ def check_rows(got, ref, mag, error, dtype, what=""):
 def same_bits(a, b, what=""):
     view = lambda t: t.contiguous().view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32) if t.is_floating_point() else t
     assert torch.equal(view(a), view(b)), what
+
+
+def rows_in_64(q, k_draft, v_draft, words, k_cache, v_cache, scale=None):
+    """citrus_tree_attn of one KV head of one document in 64 bits, all rows at once: q [G, T, d], the states [T, d] and [n, d].
+    Returns (out, lse, magnitude) as the oracle's tree_attn does, whose values they are (test_generation_cpu.py)."""
+    nodes, d = k_draft.shape
+    seen = np.array([[w >> u & 1 for u in range(nodes)] for w in words], dtype=bool)
+    real = seen.diagonal()
+    keys, values = np.concatenate([k_cache, k_draft]), np.concatenate([v_cache, v_draft])
+    s = q @ keys.T * (d ** -0.5 if scale is None else scale)
+    s[:, :, len(k_cache):] = np.where(seen, s[:, :, len(k_cache):], -np.inf)
+    s[:, ~real] = -np.inf
+    top = np.where(real[:, None], s.max(2, keepdims=True), 0.0)
+    p = np.exp(s - top)
+    total = p.sum(2, keepdims=True)
+    p /= np.where(total == 0, 1.0, total)
+    with np.errstate(divide="ignore"):
+        lse = (top + np.log(total))[..., 0]
+    return p @ values, lse, p @ np.abs(values)
+
+
+class Counts:
+    """Zero queries: a row's weights are all the same, 1 / N of the N states that it sees, and its result counts them.  V of cached state j
+    is one in a channel that goes by the state's place and its unit, or zero where `only` is given and j % 64 is another number: then a
+    channel counts a few states, one of 64 each, and each of them can be told from its absence after rounding.  Draft state u is one in a
+    channel by u."""
+
+    def __init__(self, d, only=None):
+        self.d, self.only = d, only
+
+    def channel(self, j):
+        return j // (32 if self.only is None else 64) % self.d
+
+    def cached(self, rows, unit, dtype=torch.float64, device="cpu"):
+        """V of a unit's cache."""
+        j = torch.arange(rows, device=device)
+        v = torch.zeros((rows, self.d), dtype=dtype, device=device)
+        v[j, (self.channel(j) + 5 * unit) % self.d] = (torch.ones_like(j) if self.only is None else (j % 64 == self.only)).to(dtype)
+        return v
+
+    def draft(self, nodes, unit, dtype=torch.float64, device="cpu"):
+        v = torch.zeros((nodes, self.d), dtype=dtype, device=device)
+        u = torch.arange(nodes, device=device)
+        v[u, (u + 3 * unit) % self.d] = 1
+        return v
+
+    def rows(self, n, unit, words):
+        """(result [T, d], N [T]) of nodes with these words over n cached states."""
+        nodes = len(words)
+        bits = torch.tensor([[w >> u & 1 for u in range(nodes)] for w in words], dtype=torch.float64)
+        real = bits.diagonal().clone()
+        total = (n + bits.sum(1)) * real
+        j = torch.arange(n) if self.only is None else torch.arange(self.only, max(n, self.only), 64)
+        cached = torch.bincount(self.channel(j), minlength=self.d).double()
+        count = (torch.roll(cached, 5 * unit)[None] + bits @ self.draft(nodes, unit)) * real[:, None]
+        return count / total.clamp(min=1)[:, None], total
+
+
+def check_counts(got, lse, ref, total, dtype):
+    """got [.., T, d] and lse [.., T] (optional) against Counts.rows.  The sums are whole numbers, exact in 32 bits; what is left is the
+    division (a reciprocal and a product: 2^-21 leaves room) and the result's rounding, of lse a logarithm in base 2 and a product."""
+    off = (got.double() - ref).abs()
+    most = ref * (STEP[dtype] + 2.0 ** -21)
+    assert bool((off <= most).all()), f"{int((off > most).sum())} of {off.numel()} outside"
+    if lse is not None:
+        want = torch.log(total)  # padding: -inf
+        off = torch.where(lse.double() == want, torch.zeros_like(want), (lse.double() - want).abs())
+        assert bool((off <= 2.0 ** -22 * want.abs().clamp(max=1e9)).all()), f"log-sum-exp off by up to {off.max()}"
+
+
+def heavy_places(n, seed):
+    """Places of a few heavy states among n: at edges of 32 and 64 keys, the first, the last, and some in between."""
+    rng = np.random.default_rng(seed)
+    some = {0, 31, 32, 63, 64, n // 128 * 64 - 1, n // 128 * 64, n - 1, *rng.integers(0, max(n, 1), 8).tolist()}
+    return sorted(x for x in some if 0 <= x < n)

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import paper_2406_12018_amd as api
+from generation import Counts, check_counts, check_rows, heavy_places, rows_in_64, weight_error
 from oracle import citrus_oracle as orc
 from paper_2406_12018_amd import binding as B
 
@@ -160,6 +161,65 @@ def test_a_commit_refuses_a_view_of_the_cache(kw):
 ])
 def test_bounded_decoding_refuses_a_view_of_the_cached_states(kw):
     assert evict(**kw) == B.ERR_SHAPE
+
+
+# ---- what the checks of long caches can see ----
+def states(seed, n, d, heads=2, nodes=3):
+    rng = np.random.default_rng(seed)
+    bf16 = lambda x: torch.from_numpy(x).bfloat16().double().numpy()
+    return [bf16(rng.normal(size=s) * f) for s, f in (((heads, nodes, d), 1.0), ((nodes, d), 0.5), ((nodes, d), 1.0), ((n, d), 0.5), ((n, d), 1.0))]
+
+
+def test_rows_in_64_bits_are_the_oracles():
+    q, kd, vd, kc, vc = states(1, 70, 16, nodes=6)
+    words = [0b1, 0b11, 0b101, 0, 0b10001, 0b100001]
+    for got, want in zip(rows_in_64(q, kd, vd, words, kc, vc, 0.3), orc.tree_attn(q, kd[None], vd[None], words, kc[None], vc[None], 0.3)):
+        np.testing.assert_allclose(got, want, rtol=1e-12, atol=1e-13)
+    out, lse, _ = rows_in_64(q, kd, vd, words, kc[:0], vc[:0])
+    assert np.array_equal(out[:, 0], np.broadcast_to(vd[0], (2, 16))) and (out[:, 3] == 0).all() and (lse[:, 3] == -np.inf).all()
+
+
+@pytest.mark.parametrize("n,d", [(9001, 128), (40000, 64), (131007, 128), (130000, 64)])
+def test_a_count_without_one_state_is_rejected(n, d):
+    words = [1, 3]
+    for only, lost in ((None, range(64, 96)), (0, [n // 64 * 64 - 64]), (31, [31]), (63, [n // 128 * 64 - 1])):
+        counts = Counts(d, only)
+        ref, total = counts.rows(n, 3, words)
+        right = ref.bfloat16()
+        check_counts(right, torch.log(total).float(), ref, total, "bf16")
+        v = counts.cached(n, 3)
+        wrong = ((ref * total[:, None] - v[list(lost)].sum(0)) / total[:, None]).bfloat16()  # its V was zero
+        with pytest.raises(AssertionError):
+            check_counts(wrong, None, ref, total, "bf16")
+        with pytest.raises(AssertionError):  # not seen at all, any one
+            check_counts(right, torch.log(total - 1).float(), ref, total, "bf16")
+        if only is not None:
+            moved = (ref * total[:, None] - v[lost[0]] + torch.roll(v[lost[0]], 1)) / total[:, None]  # another state's V
+            with pytest.raises(AssertionError):
+                check_counts(moved.bfloat16(), None, ref, total, "bf16")
+    ref, total = Counts(d).rows(n, 0, [1, 0])
+    assert (ref[1] == 0).all() and total[1] == 0
+
+
+@pytest.mark.parametrize("n,d", [(3000, 64), (9001, 128), (131007, 128)])
+def test_heavy_states_are_missed(n, d):
+    """Any one of them lost, or with the V of its neighbour."""
+    q, kd, vd, kc, vc = states(2, n, d)
+    words, c, places, scale = [1, 3, 5], d // 2 - 3, heavy_places(n, 10), d ** -0.5
+    q[..., c], kc[:, c], kd[:, c] = 4.0, 0.0, 0.0
+    kc[places, c] = torch.tensor(14.0 * d ** 0.5 / 4.0).bfloat16().item()
+    ref, _, mag = rows_in_64(q, kd, vd, words, kc, vc, scale)
+    error = weight_error(q, np.concatenate([kc, kd]), n + 3, scale)
+    rounded = lambda x: torch.from_numpy(x).bfloat16().double().numpy()
+    check_rows(rounded(ref), ref, mag, error, "bf16")
+    for j in places:
+        others = np.arange(n) != j
+        with pytest.raises(AssertionError):
+            check_rows(rounded(rows_in_64(q, kd, vd, words, kc[others], vc[others], scale)[0]), ref, mag, error, "bf16")
+        shifted = vc.copy()
+        shifted[j] = vc[j - 1]
+        with pytest.raises(AssertionError):
+            check_rows(rounded(rows_in_64(q, kd, vd, words, kc, shifted, scale)[0]), ref, mag, error, "bf16")
 
 
 # ---- pins of the oracle ----

@@ -193,6 +193,44 @@ def test_forms_of_the_eviction(tmp_path):
         assert status == 0 and names(launches) == want, (case, launches)
 
 
+def ranges_of(case, launch):
+    """Key ranges of an attention's launch: its workgroups in x but for the row groups."""
+    _, _, Hq, Hkv, _, T, *_ = case
+    waves, kh = (4, 4) if "f32" in launch[0] else (int(x) for x in launch[0].split("<")[1].split(",")[1:3])
+    rows = 32 * waves // kh
+    groups = (Hq // Hkv * T + rows - 1) // rows
+    assert launch[1][0] % groups == 0
+    return launch[1][0] // groups
+
+
+def test_ranges_of_the_long_caches_that_are_checked(tmp_path):
+    """The GPU's tests of long streams within a workgroup, of many ranges, and of ragged documents over several, are what they say."""
+    from test_gpu_generation_long import LENS, LONG, RAGGED
+    cases = [[*c[:7], c[7] == "f32", -1] for c in LONG]
+    cases += [[len(LENS), 1, Hq, 1, d, T, max(LENS), dtype == "f32", -1] for Hq, d, T, dtype in RAGGED]
+    wants = [c[8] for c in LONG] + [2] * len(RAGGED)
+    got, forms = in_child(tree, tmp_path, cases=cases), {}
+    for case, want, (status, launches) in zip(cases, wants, got):
+        have = ranges_of(case, launches[0])
+        assert status == 0 and (have == 1 if want == 1 else have >= want), (case, have, launches)
+        forms.setdefault(launches[0][0].split("<")[0] + launches[0][0].split("<")[1][:9], set()).add(want)
+    # one range and several of every form but the single wave's, which has one range of a few keys, and these
+    both, one = {1, 2}, {1}
+    assert {k: v & both for k, v in forms.items() if "f32" not in k} == {
+        "few_rows_kernel128, 4, 4": both, "few_rows_kernel128, 4, 2": both, "few_rows_kernel128, 8, 2": both, "few_rows_kernel128, 8, 1": both,
+        "few_rows_kernel128, 4, 1": one, "few_rows_kernel64, 4, 4,": both, "few_rows_kernel64, 4, 2,": both, "few_rows_kernel64, 8, 2,": both,
+        "few_rows_kernel64, 4, 1,": both}
+
+
+def test_kernels_of_the_bounded_steps_that_are_counted(tmp_path):
+    from test_gpu_generation_long import BOUNDED
+    wants = {"in_the_launch": [], "in_the_launch_64": [], "many_units": [], "a_unit": ["evict_unit_kernel"], "layer": ["evict_layer_kernel"]}
+    cases = [[*(c[x] for x in ("B", "L", "Hq", "Hkv", "d", "budget")), f32, int(c.get("per_layer", 0)), -1] for f32 in (False, True)
+             for c in BOUNDED.values()]
+    for name, (status, launches) in zip([*BOUNDED] * 2, in_child(evict, tmp_path, cases=cases)):
+        assert status == 0 and names(launches)[1:] == wants.get(name, ["grow_sums_kernel", "make_room_kernel"]), (name, launches)
+
+
 def test_states_beside_the_cached_rows_are_taken(tmp_path):
     """Memory that K, V and drafts share row by row, rows behind the capacity, and a token in the row that becomes its own."""
     ROW, kc, vc = 256, 1 << 24, 2 << 24
