@@ -368,6 +368,8 @@ int32_t citrus_tree_attn(const citrus_config* cfg, citrus_tensor q, citrus_tenso
  * cache_len, cache_lens  as in citrus_tree_attn
  * new_lens           optional, device int32 [B], out: len_b + accepted[b], at most cache_capacity; another array than cache_lens,
  *                    accepted and path
+ * Neither call forms sums of attention weights: where bounded steps are to follow (citrus_decode_evict_step), the caller gives the new
+ * rows' sums their values; states that enter with a sum of zero are the first to go once they are not among the recent ones.
  */
 int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citrus_tensor v_draft, int32_t draft_len,
                            const int32_t* path, int32_t path_len, const int32_t* accepted, citrus_tensor k_cache,
@@ -395,7 +397,9 @@ int32_t citrus_tree_commit(const citrus_config* cfg, citrus_tensor k_draft, citr
  * k_cache, v_cache [B, L, Hkv, >= min(tokens + 1, budget), d], in/out
  * acc            dense f32 [B, L, Hkv, cache_capacity], in/out: the states' sums
  * tokens         states that have been put into this cache so far, evicted ones included; the caller's count becomes tokens + 1.  A
- *                cache filled otherwise (by the chunk loop) starts with its number of states.
+ *                cache filled otherwise (by the chunk loop) starts with its number of states, which the budget has to hold.  One
+ *                host number for all documents: documents of different lengths (as citrus_tree_commit leaves them) take calls of their
+ *                own, and a captured call is the step of its own token, not of the next one.
  * recent         1 .. budget - start_size; the same in every step
  * evicted        optional, device, dense int32 [B, L, Hsel]: the row whose state went, -1 while the cache grows
  * workspace      >= citrus_generation_workspace_bytes(cfg, 1)

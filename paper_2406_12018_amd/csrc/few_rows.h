@@ -122,7 +122,7 @@ __device__ inline RowParts join_ranges(const FewRows& a, int64_t row, int d) {
 
 // Where a workgroup of the attention is.  grid: (row groups * key ranges, Hkv, B * L).  Workgroups go to the eight XCDs in turn, each with an
 // L2 of its own: the row groups that read the same keys are eight workgroups apart.  Next to each other, every one of them had
-// the keys from memory: seven ragged documents, 61 nodes over up to 4352 states, two row groups, 428 us, now 416.
+// the keys from memory: seven ragged documents, 61 nodes over up to 4352 states, two row groups, 550 us, now 538.
 template <bool GROUPS>  // are there several row groups, maybe?
 struct Place {
   int sp, row_group, g, b, l;

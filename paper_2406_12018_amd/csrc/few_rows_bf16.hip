@@ -10,11 +10,11 @@
 //            to 128 rows: each takes half of a stage's keys; KH = 1, four or eight blocks to a workgroup), one barrier a stage.  Four
 //            blocks have fewer stages, so that two workgroups share a compute unit, at head_dim 64 three.
 // Keys are split over workgroups where the units do not fill the chip; another launch joins the ranges.
-// Measured on an MI355X, inputs in turn from three sets: 16 ragged documents, 4 layers of 32/32 heads, head_dim 64, single tokens over up to
-// 2048 states 104.5 us = 6.7 TB/s; 13 nodes, 32/8 heads, 2 layers, over 131072 states 174 us = 6.2 TB/s; 24 nodes, 32 layers of 32/8 heads
-// over 1280 states 40 us = 4.6 TB/s with a start and an end of about 8; 61 nodes, 7 ragged documents, 8 layers of 64/8 heads over up to
-// 4352 states 416 us = 0.66 PFLOP/s, matrix pipe busy 37 % of the SIMD cycles, vector units 43 %: eight waves a compute unit do not
-// cover each other's waits.  There, two tiles a step, 128-key stages, a wave priority around the products, fewer address instructions, and one wait
+// Measured on an MI355X, a call among others, inputs in turn from three sets: 16 ragged documents, 4 layers of 32/32 heads, head_dim 64, single
+// tokens over up to 2048 states 106 us = 6.6 TB/s; 13 nodes, 32/8 heads, 2 layers, over 131072 states 176 us = 6.1 TB/s; 24 nodes, 32 layers
+// of 32/8 heads over 1280 states 42 us = 4.4 TB/s with a start and an end of about 8; 61 nodes, 7 ragged documents, 8 layers of 64/8 heads
+// over up to 4352 states 538 us = 0.51 PFLOP/s without the second words of the weights, matrix pipe busy 46 % of the SIMD cycles, vector
+// units 47 %: eight waves a compute unit do not cover each other's waits.  There, two tiles a step, 128-key stages, a wave priority around the products, fewer address instructions, and one wait
 // for all of a tile's reads of LDS changed nothing.  A launch of one tile takes 7.7 us: reads that depend on each other, and instructions that no one has fetched yet.
 #include "evict_unit.h"
 #include "key_stream.h"

@@ -3,8 +3,8 @@
 // The f32 mode is for tests and small models.  A wave takes 32 rows and 32-key tiles of its own, S^T = K.Q^T and O^T = V^T.P^T, straight
 // from global memory: the weights leave the first product in the layout that the second reads, so nothing goes through LDS before
 // the waves join.  K of the next tile is on its way during the second product, V during the first.  88 layers of 64/8 heads over 854
-// states, one row: head_dim 128 131 us = 4.7 TB/s, head_dim 64 84 us = 3.7 TB/s (two waves a SIMD, 32 columns of a product for 8 rows);
-// with 16 rows, four row groups, 254 us.  Loads marked as not to be kept were slower (each 16-byte piece of a key is a load of its own).
+// states, one node: head_dim 128 128 us = 4.8 TB/s, head_dim 64 75 us = 4.1 TB/s (two waves a SIMD, 32 columns of a product for 8 rows);
+// with 16 nodes, four row groups, 229 us.  Loads marked as not to be kept were slower (each 16-byte piece of a key is a load of its own).
 #include "evict_unit.h"
 
 namespace citrus {

@@ -24,7 +24,13 @@ __global__ __launch_bounds__(256) void join_ranges_kernel(FewRows a) {
   finish_row<E>(a, b, l, h, t, row, d, p, real);
 }
 
-constexpr int kMostSplits = 64, kFewKeys = 512;
+// Ranges of keys, at most: one KV head, 4 rows over 16000 states 19.6 us (32: 16.8, 128: 30.7), over 130000 38.2 (48.8, 39.9); four units of
+// 160 rows over 60000 66 (86, 66).
+constexpr int kMostSplits = 64;
+constexpr int kFewKeys = 512;
+// Keys of a range, at least: 8 KV heads over 832 states, 32 rows 10.8 us (64: 12.2, 256: 12.4), 96 rows 14.9 (16.2, 15.4), but 424 rows 42.6
+// (27.2, 42.6); one KV head, 4 rows over 4000 states 12.7 (18.2, 11.3).
+constexpr int kLeastKeys = 128;
 // Workgroups of a form that the chip holds.
 int64_t slots_of(int dtype, const Dims& dm, const FewRowsPlan& p) {
   if (dm.D == 128) return p.waves == 4 && p.kh == 1 ? 512 : 256;  // LDS; in f32 registers
@@ -33,10 +39,10 @@ int64_t slots_of(int dtype, const Dims& dm, const FewRowsPlan& p) {
 
 // More than 64 rows, a block of 32 to a wave: four waves and few stages in LDS leave room for two workgroups to a compute unit, at head_dim
 // 64 for three; eight waves only for one.  head_dim 64: 16 documents, 16 layers of 8 KV heads, 124 rows over 300 states 97.5 and 60.5 us (four
-// waves); 3 documents, 8 KV heads, 427 rows over 14000 states 100 and 87.  head_dim 128: 2560 units of 124 rows over 60, 300, 1200 states 127
-// and 79, 196 and 144, 437 and 394; 288 of them over 4000 states 186 and 171; of 427 rows over 60, 300, 1200 states 326 and 261, 474 and 420,
-// 1012 and 1014, over 4000 states (512 units) 581 and 594; of 160 rows, where half of the second workgroup's waves would have no
-// rows, 136 and 141.  Few units of up to 128 rows keep the shorter chain of eight waves that halve a stage (head_dim 64, 300 states, 13.1 and 14.9).
+// waves); 3 documents, 8 KV heads, 427 rows over 14000 states 100 and 87.  head_dim 128: 2560 units of 120 rows over 60, 300, 1200 states 108
+// and 76, 173 and 132, 442 and 378; 288 of them over 4000 states 193 and 165; of 424 rows over 60, 300, 500 states 347 and 273, 533 and 486,
+// 682 and 650; over 700, 1200, 4000 states (of the last 512 units) 848 and 818, 1284 and 1250, 737 and 733, and of 160 rows over 300 states,
+// where half of the second workgroup's waves have no rows, 224 and 206: these stay with eight.  Few units of up to 128 rows keep the shorter chain of eight waves that halve a stage (head_dim 64, 300 states, 13.1 and 14.9).
 FewRowsPlan form_of(int dtype, const Dims& dm, int nodes, int keys, bool logits) {
   const int blocks = (dm.G * nodes + 31) / 32;
   FewRowsPlan p{};
@@ -74,7 +80,7 @@ FewRowsPlan plan_for(int dtype, const Dims& dm, int nodes, int most_keys, bool l
   int64_t best = INT64_MAX;
   for (int s = 1; s <= most_splits(dtype, dm, p); ++s) {
     const int per = (tiles + s - 1) / s;
-    if (s > 1 && per * unit < 128) break;
+    if (s > 1 && per * unit < kLeastKeys) break;
     if ((tiles + per - 1) / per != s) continue;  // no empty ranges
     const bool evicts = may_evict && s == 1;
     const int64_t rounds = (s * groups + slots - 1) / slots, each = per * unit / 32 * tile + 6 + (evicts ? 6 : 0) + (s > 1 ? rows / 16 : 0);
